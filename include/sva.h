@@ -397,6 +397,200 @@ int sva_sparse_attention_fp8(const sva_problem* prob, const sva_fp8_tensors* in,
 int sva_dense_attention_fp8(const sva_problem* prob, const sva_fp8_tensors* in, void* out, float* lse,
                             void* stream);
 
+/* ---- Rotary positions, a quantised key/value cache and attention over it:
+ * generation step by step (a streaming video model that keeps the tokens of
+ * earlier frames, the text model in front of the denoiser), next to the
+ * whole-sequence operators above.  These take tensors [B, H, N, D] by their
+ * strides, so that a slice of a fused projection's [B, N, H, D] is taken as it
+ * lies. ---- */
+
+/* One tensor [B, H, N, D]: element (b, h, n, d) at data + b*stride_b +
+ * h*stride_h + n*stride_n + d, strides in elements, >= 0.  An input may
+ * repeat itself (stride 0); an output's rows must not overlap. */
+typedef struct sva_heads {
+  void* data;
+  int32_t heads;
+  int64_t stride_b, stride_h, stride_n;
+} sva_heads;
+
+typedef enum sva_rotary_layout {
+  SVA_ROTARY_HALF = 0,        /* pair i of a row: (x[i], x[i + rot_dim/2])           */
+  SVA_ROTARY_INTERLEAVED = 1  /* pair i of a row: (x[2i], x[2i + 1])                 */
+} sva_rotary_layout;
+
+/* How the frequencies f_i = base^(-2i/rot_dim), i < rot_dim/2, are scaled by a
+ * factor s >= 1 for contexts s times as long as the trained ones. */
+typedef enum sva_rotary_scaling {
+  SVA_ROTARY_PLAIN = 0,       /* f_i (factor is not read)                            */
+  SVA_ROTARY_LINEAR = 1,      /* f_i / s: positions interpolated                     */
+  SVA_ROTARY_NTK = 2,         /* base * s^(rot_dim/(rot_dim-2)) in place of base     */
+  SVA_ROTARY_YARN = 3         /* by parts (Peng et al. 2023): with the turns
+                                 r_i = original_len * f_i / 2pi that pair i makes over
+                                 the trained context and g_i = (r_i - beta_slow) /
+                                 (beta_fast - beta_slow) clamped to [0, 1],
+                                 (1 - g_i) f_i / s + g_i f_i                         */
+} sva_rotary_scaling;
+
+typedef struct sva_rotary_spec {
+  int32_t rot_dim;       /* channels turned, even, in [2, 512]                      */
+  int32_t scaling;       /* sva_rotary_scaling                                      */
+  double base;           /* finite, > 1                                             */
+  double factor;         /* s, finite, >= 1                                         */
+  double original_len;   /* YARN: trained context, finite, > 0                      */
+  double beta_fast;      /* YARN: finite, > beta_slow (e.g. 32)                     */
+  double beta_slow;      /* YARN: finite, >= 0 (e.g. 1)                             */
+  double magnitude;      /* factor on cosine and sine, finite; <= 0 selects 1, or
+                            0.1 ln(s) + 1 with YARN                                 */
+} sva_rotary_spec;
+
+/* The scaled frequencies, radians per position (float64 [rot_dim/2], HOST
+ * memory; a program copies them to the device once), and the magnitude.  Host
+ * only. */
+int sva_rotary_frequencies(const sva_rotary_spec* spec, double* freq, double* magnitude);
+
+typedef struct sva_rotary_params {
+  int32_t batch, tokens; /* B >= 1, N >= 1                                          */
+  int32_t head_dim;      /* D in [2, 1024]                                          */
+  int32_t rot_dim;       /* even, in [2, min(D, 512)]: the row's first channels     */
+  int32_t layout;        /* sva_rotary_layout                                       */
+  int32_t dtype;         /* sva_dtype of every tensor                               */
+  int32_t backward;      /* nonzero: the transposed map, which takes gradients of
+                            the outputs to gradients of the inputs                  */
+  double magnitude;      /* m, finite (from sva_rotary_frequencies)                 */
+} sva_rotary_params;
+
+/* Rotary positions of Q and K in one launch.  Pair (a, b) number i of a token
+ * at position p becomes m (a cos t - b sin t, a sin t + b cos t) with t = p f_i
+ * (backward: t = -p f_i); channels from rot_dim on are copied.
+ *   freq       : float64 [rot_dim/2] device, 8-byte aligned
+ *   positions  : int32 device, token (b, n) at positions[b * pos_stride_b + n],
+ *                any sign; pos_stride_b 0 shares one row of positions
+ *   q_in, q_out: the tensor and its result, q_out->heads == q_in->heads; q_out
+ *                may be q_in (same data and strides: in place, where only the
+ *                rot_dim channels are read and written) and must otherwise lie
+ *                apart from it
+ *   k_in, k_out: the same for K with its own head count, or both NULL
+ * Outputs must not share memory with each other or with the other tensor's
+ * input (slices of one buffer may interleave).  The angle is formed and
+ * reduced modulo one turn in float64, cosine, sine and the products in
+ * float32, each result rounded once.  Data aligned to their elements; tensors
+ * whose data and strides are multiples of 16 bytes (rot_dim of 8 elements in
+ * bf16 or 4 in float32, twice that in the half layout) take 16-byte accesses. */
+int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* positions,
+               int64_t pos_stride_b, const sva_heads* q_in, const sva_heads* q_out,
+               const sva_heads* k_in, const sva_heads* k_out, void* stream);
+
+/* Formats of a cache.  One scale per token and head, apart for K and V: an
+ * element is its code times its row's scale.  With a the row's largest
+ * magnitude:
+ *   e4m3  OCP e4m3 byte; scale 2^e, the smallest e in [-127, 127] with
+ *         a <= 448 * 2^e (e = 0 for a = 0), as sva_quantize_fp8 chooses it;
+ *         x * 2^-e is rounded to nearest, ties to even
+ *   int8  scale a / 127 rounded to float32 (1 where that is zero); the exact
+ *         quotient x / scale is rounded to nearest, ties to even (and kept
+ *         within +-127)
+ *   bf16  the element itself, no scales
+ * A row with Inf or NaN gets unspecified codes and scale (bf16: itself). */
+typedef enum sva_cache_format {
+  SVA_CACHE_BF16 = 0,
+  SVA_CACHE_E4M3 = 1,
+  SVA_CACHE_INT8 = 2
+} sva_cache_format;
+
+/* A paged cache in device memory that the caller owns.  A slot is page *
+ * page_size + place in the page. */
+typedef struct sva_cache {
+  int32_t format;        /* sva_cache_format                                        */
+  int32_t num_pages;     /* >= 1; num_pages * page_size <= INT32_MAX                */
+  int32_t kv_heads;      /* Hkv >= 1                                                */
+  int32_t page_size;     /* tokens per page: 16, 32, 64, 128 or 256                 */
+  int32_t head_dim;      /* D in {64, 112, 128}                                     */
+  void* k;               /* [num_pages, Hkv, page_size, D] codes, 16-byte aligned   */
+  void* v;               /* the same for V                                          */
+  float* k_scale;        /* [num_pages, Hkv, page_size], 16-byte aligned (bf16: not
+                            read, may be NULL)                                      */
+  float* v_scale;
+} sva_cache;
+
+/* Quantise the rows of N new tokens per batch entry into their slots.
+ *   dtype : sva_dtype of k and v ([B, Hkv, N, D]; 16-byte aligned data and strides)
+ *   slots : int32 device, token (b, n) goes to slots[b * slots_stride_b + n]; a
+ *           value outside [0, num_pages * page_size) writes nothing (padding,
+ *           rejected drafts).  The others must differ from each other: where
+ *           two tokens name one slot its codes and scale may be of either.
+ * Slots that are not named keep their contents. */
+int sva_cache_write(const sva_cache* cache, int32_t batch, int32_t tokens, int32_t dtype,
+                    const sva_heads* k, const sva_heads* v, const int32_t* slots,
+                    int64_t slots_stride_b, void* stream);
+
+/* The tokens at these slots back as K and V, code times scale in float32,
+ * rounded once to dtype (a slot may be named any number of times; one out of
+ * range gives zeros).  k, v: outputs [B, Hkv, N, D] as above (contiguous ones
+ * are what the whole-sequence operators take). */
+int sva_cache_read(const sva_cache* cache, int32_t batch, int32_t tokens, int32_t dtype,
+                   const int32_t* slots, int64_t slots_stride_b, const sva_heads* k,
+                   const sva_heads* v, void* stream);
+
+#define SVA_CACHE_MAX_QUERIES 1024
+
+/* A step's queries: T drafted tokens per batch entry (one for plain decoding). */
+typedef struct sva_cache_query {
+  int32_t batch;         /* B in [1, 65536]                                         */
+  int32_t heads;         /* H, a multiple of the cache's Hkv; query head h reads
+                            cache head h / (H / Hkv)                                */
+  int32_t queries;       /* T in [1, SVA_CACHE_MAX_QUERIES]                         */
+  int32_t max_pages;     /* columns of the page table, >= 1                         */
+  double softmax_scale;  /* c; <= 0 selects 1/sqrt(D)                               */
+  int32_t out_dtype;     /* sva_dtype of out                                        */
+} sva_cache_query;
+
+/* Bytes of device workspace that sva_cache_attention needs (partial results of
+ * keys divided among workgroups, at most 36 MB; the cache's pointers are not
+ * read).  Host only. */
+int sva_cache_attention_workspace(const sva_cache* cache, const sva_cache_query* query, size_t* bytes);
+
+/* Attention of drafted tokens over a cache and over each other: query token t
+ * of head h of batch entry b attends to
+ *   the cached tokens 0 .. lengths[b]-1, token j in slot
+ *     page_table[b][j / page_size] * page_size + j % page_size, and
+ *   the drafted tokens s < T with mask[b][t][s] != 0 (a tree: t itself and its
+ *     ancestors; any other pattern is taken as it is),
+ * and gets the softmax-weighted mean of their values (weights softmax(c q.k)).
+ *   q          : bf16 [B, H, T, D]
+ *   page_table : int32 [B, max_pages] device; tokens of a page outside
+ *                [0, num_pages) are skipped
+ *   lengths    : int32 [B] device, clamped to [0, max_pages * page_size]; what
+ *                lies in slots behind a length does not matter
+ *   k_new,v_new: bf16 [B, Hkv, T, D], keys and values of the drafted tokens
+ *                (not in the cache yet: sva_cache_write takes the accepted
+ *                ones), or both NULL: queries see the cache alone
+ *   mask       : uint8 device, (b, t, s) at mask[b * mask_stride_b + t * T + s],
+ *                mask_stride_b 0 shares one mask; NULL: token t sees s <= t
+ *   counts     : int32 [B] device or NULL: the drafted tokens that entry b has,
+ *                clamped to [0, T]; those behind it are neither keys nor
+ *                queries, and their rows of out and lse are left as they were
+ *   out        : [B, H, T, D], bf16 or float32; zeros for a query that attends
+ *                to nothing
+ *   lse        : float32 [B, H, T] contiguous or NULL; natural-log log-sum-exp of
+ *                the scaled logits (-inf for a query that attends to nothing)
+ *   workspace  : device memory, 256-byte aligned, at least
+ *                sva_cache_attention_workspace bytes; contents on entry do not
+ *                matter.  Calls that share one must not overlap.
+ * q, k_new, v_new and out: 16-byte aligned data and strides.  Masked keys and
+ * values take no part, whatever they hold.  Codes are widened to bf16 exactly
+ * and multiplied by bf16 MFMA with float32 accumulation, the scales applied to
+ * logits and weights in float32, with a running maximum.  For a bf16 result
+ * the weights are rounded to bf16 before the product with V; for a float32
+ * result they are carried as a sum of two bf16 values.  The keys of all
+ * sequences are divided evenly among workgroups, so the order in which a
+ * query's partial results are added, and with it its last bits, depends on the
+ * lengths in the call; the same call gives the same bits. */
+int sva_cache_attention(const sva_cache* cache, const sva_cache_query* query, const sva_heads* q,
+                        const int32_t* page_table, const int32_t* lengths, const sva_heads* k_new,
+                        const sva_heads* v_new, const uint8_t* mask, int64_t mask_stride_b,
+                        const int32_t* counts, void* workspace, size_t workspace_bytes,
+                        const sva_heads* out, float* lse, void* stream);
+
 /* Static text for a status code. */
 const char* sva_status_string(int status);
 

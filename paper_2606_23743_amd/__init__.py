@@ -12,7 +12,8 @@ from ._lib import (SvaError, Problem, SelectParams, RopeParams, load, problem, p
                    status_string, LIB_PATH, Tokens, tokens, token_keep_count, token_select, token_select_noalloc,
                    token_gather, token_scatter, token_select_workspace, Fp8Tensors, fp8_padded_len, fp8_code_dim,
                    quantize_fp8, sparse_attention_fp8, dense_attention_fp8, remainder_workspace,
-                   block_moments, sparse_attention_remainder)
+                   block_moments, sparse_attention_remainder, rotary_frequencies, rotary_plan, rotary, kv_cache,
+                   cache_write, cache_read, cache_attention_workspace, cache_attention)
 
 __all__ = [
     "workloads", "SvaError", "Problem", "SelectParams", "RopeParams", "load", "problem",
@@ -21,5 +22,6 @@ __all__ = [
     "status_string", "LIB_PATH", "Tokens", "tokens", "token_keep_count", "token_select", "token_select_noalloc",
     "token_gather", "token_scatter", "token_select_workspace", "Fp8Tensors", "fp8_padded_len", "fp8_code_dim",
     "quantize_fp8", "sparse_attention_fp8", "dense_attention_fp8", "remainder_workspace",
-    "block_moments", "sparse_attention_remainder",
+    "block_moments", "sparse_attention_remainder", "rotary_frequencies", "rotary_plan", "rotary", "kv_cache",
+    "cache_write", "cache_read", "cache_attention_workspace", "cache_attention",
 ]

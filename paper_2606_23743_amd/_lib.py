@@ -18,6 +18,10 @@ SVA_OK, SVA_ERR_INVALID_ARG, SVA_ERR_SHAPE, SVA_ERR_ALIGNMENT, SVA_ERR_UNSUPPORT
 SVA_BF16, SVA_F32 = 0, 1
 SVA_SELECT_TOPK, SVA_SELECT_CUMMASS = 0, 1
 SVA_SELECT_MAX_BLOCKS = 2048
+SVA_ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+SVA_ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+SVA_CACHE_FORMATS = {"bf16": 0, "e4m3": 1, "int8": 2}
+SVA_CACHE_MAX_QUERIES = 1024
 
 
 class SvaError(RuntimeError):
@@ -53,6 +57,34 @@ class SelectParams(ctypes.Structure):
                 ("force_first_frame", ctypes.c_int32)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("heads", ctypes.c_int32), ("stride_b", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+
+
+class RotarySpec(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_len", ctypes.c_double), ("beta_fast", ctypes.c_double),
+                ("beta_slow", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("backward", ctypes.c_int32), ("magnitude", ctypes.c_double)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class CacheQuery(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("queries", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("softmax_scale", ctypes.c_double), ("out_dtype", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -68,6 +100,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib = ctypes.CDLL(path)
     P, S = ctypes.POINTER(Problem), ctypes.POINTER(SelectParams)
     vp, i32p = ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32)
+    i32, i64, HP, CP = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(Heads), ctypes.POINTER(Cache)
     sig = {
         "sva_num_blocks": [P, i32p],
         "sva_max_keep": [P, S, i32p],
@@ -93,6 +126,14 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "sva_quantize_fp8": [P, vp, vp, vp, ctypes.POINTER(Fp8Tensors), vp],
         "sva_sparse_attention_fp8": [P, ctypes.POINTER(Fp8Tensors), vp, vp, ctypes.c_int32, vp, vp, vp],
         "sva_dense_attention_fp8": [P, ctypes.POINTER(Fp8Tensors), vp, vp, vp],
+        "sva_rotary_frequencies": [ctypes.POINTER(RotarySpec), ctypes.POINTER(ctypes.c_double),
+                                   ctypes.POINTER(ctypes.c_double)],
+        "sva_rotary": [ctypes.POINTER(RotaryParams), vp, vp, i64, HP, HP, HP, HP, vp],
+        "sva_cache_write": [CP, i32, i32, i32, HP, HP, vp, i64, vp],
+        "sva_cache_read": [CP, i32, i32, i32, vp, i64, HP, HP, vp],
+        "sva_cache_attention_workspace": [CP, ctypes.POINTER(CacheQuery), ctypes.POINTER(ctypes.c_size_t)],
+        "sva_cache_attention": [CP, ctypes.POINTER(CacheQuery), HP, vp, vp, HP, HP, vp, i64, vp, vp,
+                                ctypes.c_size_t, HP, vp, vp],
         "sva_status_string": [ctypes.c_int],
         "sva_version": [],
     }
@@ -687,3 +728,299 @@ def token_scatter(y_kept, kept_pos, base, out=None, stream=None):
                                     _ptr(base), _ptr(out), _stream(stream)), "sva_token_scatter")
     _record(stream, y_kept, kept_pos, base, out)
     return out
+
+
+# ------------------------------------- rotary positions, the key/value cache
+
+def _device_of(t, name):
+    """Calls launch on the current device's streams: its tensors have to be there."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _heads(t, dtype, shape, name) -> Heads:
+    """A tensor [B, H, N, D] with any strides, its channels contiguous."""
+    _device_of(t, name)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    sb, sh, sn, sd = t.stride()
+    if sd != 1 and shape[3] > 1:
+        raise ValueError(f"{name}'s channels must be contiguous (stride 1), got stride {sd}")
+    return Heads(t.data_ptr(), shape[1], sb, sh, sn)
+
+
+def _rows_of_ints(t, batch, columns, name):
+    """int32 [batch, columns] or [columns] (shared): its pointer and batch stride."""
+    torch = _torch()
+    _device_of(t, name)
+    if t.dtype != torch.int32:
+        raise TypeError(f"{name} must be {torch.int32}, got {t.dtype}")
+    if t.dim() == 1 and t.shape[0] == columns:
+        step, stride = t.stride(0), 0
+    elif t.dim() == 2 and t.shape[0] == batch and t.shape[1] == columns:
+        stride, step = t.stride()
+    else:
+        raise ValueError(f"{name} must have shape {(batch, columns)} or {(columns,)}, got {tuple(t.shape)}")
+    if step != 1 and columns > 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return t.data_ptr(), stride
+
+
+def _dtype_code(dtype, name):
+    torch = _torch()
+    if dtype == torch.bfloat16 or dtype == "bf16":
+        return torch.bfloat16, SVA_BF16
+    if dtype == torch.float32 or dtype in ("f32", "float32"):
+        return torch.float32, SVA_F32
+    raise TypeError(f"{name} must be bfloat16 or float32, got {dtype}")
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                       original_len: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                       magnitude: float = 0.0) -> Tuple:
+    """(list of rot_dim / 2 frequencies in radians per position, factor on cosine
+    and sine), sva_rotary_frequencies.  scaling: "none", "linear", "ntk" or
+    "yarn"; factor: how many times longer the contexts are; original_len: the
+    trained one ("yarn")."""
+    if scaling not in SVA_ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(SVA_ROTARY_SCALINGS)}, got {scaling!r}")
+    spec = RotarySpec(int(rot_dim), SVA_ROTARY_SCALINGS[scaling], float(base), float(factor), float(original_len),
+                      float(beta_fast), float(beta_slow), float(magnitude))
+    freq = (ctypes.c_double * max(1, int(rot_dim) // 2))()
+    mag = ctypes.c_double()
+    _check(load().sva_rotary_frequencies(ctypes.byref(spec), freq, ctypes.byref(mag)), "sva_rotary_frequencies")
+    return list(freq), mag.value
+
+
+def rotary_plan(head_dim: int, rot_dim: Optional[int] = None, layout: str = "half", base: float = 10000.0,
+                scaling: str = "none", factor: float = 1.0, original_len: float = 0.0, beta_fast: float = 32.0,
+                beta_slow: float = 1.0, magnitude: float = 0.0, device="cuda") -> dict:
+    """What rotary() turns by, made once: {head_dim, rot_dim, layout, magnitude,
+    freq (float64 [rot_dim / 2] on the device)}.  rot_dim: the channels turned,
+    the first of each head (all when None); layout: "half" (pairs i, i + rot_dim/2)
+    or "interleaved" (pairs 2i, 2i + 1); the rest as in rotary_frequencies."""
+    if layout not in SVA_ROTARY_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(SVA_ROTARY_LAYOUTS)}, got {layout!r}")
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    if rot_dim > head_dim:
+        raise ValueError(f"rot_dim {rot_dim} exceeds head_dim {head_dim}")
+    freq, mag = rotary_frequencies(rot_dim, base, scaling, factor, original_len, beta_fast, beta_slow, magnitude)
+    torch = _torch()
+    return {"head_dim": int(head_dim), "rot_dim": int(rot_dim), "layout": layout, "magnitude": mag,
+            "freq": torch.tensor(freq, dtype=torch.float64, device=device)}
+
+
+def rotary(plan: dict, positions, q, k=None, q_out=None, k_out=None, backward: bool = False, stream=None) -> Tuple:
+    """Rotary positions of q [B, H, N, D] and, in the same launch, k [B, Hk, N, D]
+    (bf16 or float32, any strides with contiguous channels: a slice of a fused
+    projection is taken as it lies), sva_rotary.  positions: int32 [B, N], or [N]
+    for all entries.  q_out / k_out may be q / k (in place).  backward: the
+    transposed map, from gradients of the outputs to gradients of the inputs.
+    Returns (q_out, k_out), k_out None without k."""
+    torch = _torch()
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a tensor [B, H, N, D]")
+    B, H, N, D = q.shape
+    if D != plan["head_dim"]:
+        raise ValueError(f"q has {D} channels, the plan {plan['head_dim']}")
+    dt, code = _dtype_code(q.dtype, "q")
+    qi = _heads(q, dt, q.shape, "q")
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    qo = _heads(q_out, dt, q.shape, "q_out")
+    ki = ko = None
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k must be a tensor [B, H, N, D]")
+        shp = torch.Size((B, k.shape[1], N, D))
+        ki = _heads(k, dt, shp, "k")
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        ko = _heads(k_out, dt, shp, "k_out")
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    freq = plan["freq"]
+    _device_of(freq, "plan['freq']")
+    pos, pos_b = _rows_of_ints(positions, B, N, "positions")
+    prm = RotaryParams(B, N, D, plan["rot_dim"], SVA_ROTARY_LAYOUTS[plan["layout"]], code, 1 if backward else 0,
+                       plan["magnitude"])
+    _check(load().sva_rotary(prm, freq.data_ptr(), pos, pos_b, qi, qo, ki, ko, _stream(stream)), "sva_rotary")
+    _record(stream, q, k, q_out, k_out, freq, positions)
+    return q_out, k_out
+
+
+def kv_cache(num_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, fmt: str = "e4m3",
+             device="cuda") -> dict:
+    """An empty paged cache: {k, v: [num_pages, kv_heads, page_size, head_dim]
+    codes (bfloat16, uint8 e4m3 bytes or int8, as fmt is "bf16", "e4m3" or
+    "int8"), k_scale, v_scale: float32 [num_pages, kv_heads, page_size], None for
+    bf16}.  Any tensors of these shapes and types are a cache."""
+    torch = _torch()
+    if fmt not in SVA_CACHE_FORMATS:
+        raise ValueError(f"fmt must be one of {sorted(SVA_CACHE_FORMATS)}, got {fmt!r}")
+    dt = {"bf16": torch.bfloat16, "e4m3": torch.uint8, "int8": torch.int8}[fmt]
+    shp = (int(num_pages), int(kv_heads), int(page_size), int(head_dim))
+    cache = {n: torch.zeros(shp, dtype=dt, device=device) for n in ("k", "v")}
+    for n in ("k_scale", "v_scale"):
+        cache[n] = None if fmt == "bf16" else torch.zeros(shp[:3], dtype=torch.float32, device=device)
+    return cache
+
+
+def _cache(c: dict) -> Cache:
+    torch = _torch()
+    k, v = c["k"], c["v"]
+    _device_of(k, "cache['k']")
+    fmt = {torch.bfloat16: 0, torch.uint8: 1, torch.int8: 2}.get(k.dtype)
+    if fmt is None:
+        raise TypeError(f"cache['k'] must be bfloat16, uint8 (e4m3) or int8, got {k.dtype}")
+    if k.dim() != 4:
+        raise ValueError("cache['k'] must be [pages, kv_heads, page_size, head_dim]")
+    shp = k.shape
+    _need(k, k.dtype, shp, "cache['k']")
+    _need(v, k.dtype, shp, "cache['v']")
+    _device_of(v, "cache['v']")
+    ks = vs = None
+    if fmt:
+        ks, vs = c["k_scale"], c["v_scale"]
+        _need(ks, torch.float32, shp[:3], "cache['k_scale']")
+        _need(vs, torch.float32, shp[:3], "cache['v_scale']")
+        _device_of(ks, "cache['k_scale']")
+        _device_of(vs, "cache['v_scale']")
+        ks, vs = ks.data_ptr(), vs.data_ptr()
+    return Cache(fmt, shp[0], shp[1], shp[2], shp[3], k.data_ptr(), v.data_ptr(), ks, vs)
+
+
+def cache_write(cache: dict, k, v, slots, stream=None) -> dict:
+    """Quantise the rows of k and v (bf16 or float32 [B, kv_heads, N, D], any
+    strides with contiguous channels) into slots (int32 [B, N]; page * page_size +
+    place; out of range: nothing is written; the others distinct),
+    sva_cache_write.  Returns the cache."""
+    torch = _torch()
+    st = _cache(cache)
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("k must be a tensor [B, kv_heads, N, D]")
+    dt, code = _dtype_code(k.dtype, "k")
+    B, _, N, _ = k.shape
+    shp = torch.Size((B, st.kv_heads, N, st.head_dim))
+    hk, hv = _heads(k, dt, shp, "k"), _heads(v, dt, shp, "v")
+    if slots.dim() == 1 and B > 1:
+        raise ValueError("slots must be [B, N]: entries cannot share slots")
+    ptr, sb = _rows_of_ints(slots, B, N, "slots")
+    _check(load().sva_cache_write(st, B, N, code, hk, hv, ptr, sb, _stream(stream)), "sva_cache_write")
+    _record(stream, k, v, slots, *cache.values())
+    return cache
+
+
+def cache_read(cache: dict, slots, k=None, v=None, dtype="bf16", stream=None) -> Tuple:
+    """The tokens at slots (int32 [B, N]; out of range: zeros) as K and V
+    [B, kv_heads, N, D] of dtype ("bf16" or "f32"), sva_cache_read; contiguous
+    where allocated here, as the whole-sequence operators take them."""
+    torch = _torch()
+    st = _cache(cache)
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 2:
+        raise ValueError("slots must be a tensor [B, N]")
+    B, N = slots.shape
+    dt, code = _dtype_code(dtype, "dtype")
+    shp = torch.Size((B, st.kv_heads, N, st.head_dim))
+    ptr, sb = _rows_of_ints(slots, B, N, "slots")
+    if k is None:
+        k = torch.empty(shp, dtype=dt, device=slots.device)
+    if v is None:
+        v = torch.empty(shp, dtype=dt, device=slots.device)
+    _check(load().sva_cache_read(st, B, N, code, ptr, sb, _heads(k, dt, shp, "k"), _heads(v, dt, shp, "v"),
+                                 _stream(stream)), "sva_cache_read")
+    _record(stream, k, v, slots, *cache.values())
+    return k, v
+
+
+def cache_attention_workspace(cache: dict, batch: int, heads: int, queries: int, max_pages: int) -> int:
+    """Workspace bytes of cache_attention for B = batch, H = heads, T = queries and
+    a page table of max_pages columns (sva_cache_attention_workspace)."""
+    out = ctypes.c_size_t(0)
+    _check(load().sva_cache_attention_workspace(_cache(cache), CacheQuery(batch, heads, queries, max_pages, 0.0, SVA_BF16),
+                                                ctypes.byref(out)), "sva_cache_attention_workspace")
+    return out.value
+
+
+def cache_attention(cache: dict, q, page_table, lengths, k_new=None, v_new=None, mask=None, counts=None,
+                    softmax_scale: float = 0.0, out_dtype="bf16", out=None, want_lse: bool = False, lse=None,
+                    workspace=None, stream=None) -> Tuple:
+    """Attention of T drafted tokens per entry (one in plain decoding), q bf16
+    [B, H, T, D], over the cached tokens that page_table (int32 [B, max_pages]) and
+    lengths (int32 [B]) name and over each other, sva_cache_attention.  k_new,
+    v_new: bf16 [B, kv_heads, T, D]; mask: uint8 or bool [B, T, T] or [T, T], token
+    t sees drafted token s where mask[b, t, s] is not zero (None: s <= t); counts:
+    int32 [B], the drafted tokens an entry has (None: T).  q, k_new, v_new and out
+    take any strides with contiguous channels that are multiples of 16 bytes; out
+    is made like q, of out_dtype ("bf16" or "f32").  workspace: a uint8 device
+    tensor of cache_attention_workspace bytes (allocated when None).  Returns
+    (out, lse)."""
+    torch = _torch()
+    st = _cache(cache)
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a tensor [B, H, T, D]")
+    B, H, T, D = q.shape
+    if D != st.head_dim:
+        raise ValueError(f"q has {D} channels, the cache {st.head_dim}")
+    hq = _heads(q, torch.bfloat16, q.shape, "q")
+    _need(lengths, torch.int32, (B,), "lengths")
+    _device_of(lengths, "lengths")
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be a tensor [B, max_pages]")
+    _need(page_table, torch.int32, (B, page_table.shape[1]), "page_table")
+    _device_of(page_table, "page_table")
+    hk = hv = None
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new go together")
+    if k_new is not None:
+        shp = torch.Size((B, st.kv_heads, T, D))
+        hk, hv = _heads(k_new, torch.bfloat16, shp, "k_new"), _heads(v_new, torch.bfloat16, shp, "v_new")
+    mask_b = 0
+    if mask is not None:
+        if k_new is None:
+            raise ValueError("mask without drafted keys")
+        _device_of(mask, "mask")
+        if mask.dtype not in (torch.uint8, torch.bool):
+            raise TypeError(f"mask must be uint8 or bool, got {mask.dtype}")
+        if mask.shape not in ((B, T, T), (T, T)):
+            raise ValueError(f"mask must have shape {(B, T, T)} or {(T, T)}, got {tuple(mask.shape)}")
+        if mask.stride(-1) != 1 and T > 1 or mask.stride(-2) != T and T > 1:
+            raise ValueError("mask's last two dimensions must be contiguous")
+        mask_b = mask.stride(0) if mask.dim() == 3 else 0
+    if counts is not None:
+        _need(counts, torch.int32, (B,), "counts")
+        _device_of(counts, "counts")
+    if out is None:
+        dt, code = _dtype_code(out_dtype, "out_dtype")
+        out = torch.empty_like(q, dtype=dt)
+    else:
+        dt, code = _dtype_code(out.dtype, "out")
+    ho = _heads(out, dt, q.shape, "out")
+    if want_lse and lse is None:
+        lse = torch.empty((B, H, T), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _need(lse, torch.float32, (B, H, T), "lse")
+        _device_of(lse, "lse")
+    qry = CacheQuery(B, H, T, page_table.shape[1], float(softmax_scale), code)
+    lib = load()
+    if workspace is None:
+        need = ctypes.c_size_t(0)
+        _check(lib.sva_cache_attention_workspace(st, qry, ctypes.byref(need)), "sva_cache_attention_workspace")
+        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    else:
+        _device_of(workspace, "workspace")
+    ws_ptr, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    _check(lib.sva_cache_attention(st, qry, hq, page_table.data_ptr(), lengths.data_ptr(), hk, hv, _ptr(mask), mask_b,
+                                   _ptr(counts), ws_ptr, ws_bytes, ho, _ptr(lse), _stream(stream)),
+           "sva_cache_attention")
+    _record(stream, q, page_table, lengths, k_new, v_new, mask, counts, workspace, out, lse, *cache.values())
+    return out, lse

@@ -1,0 +1,75 @@
+// Arguments of the rotary, cache and cache-attention kernels after host
+// validation (strides in elements).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sva {
+
+struct HeadsView {
+  void* p;
+  int64_t sb, sh, sn;
+  int heads;
+};
+
+// rotary.hip
+struct RotaryArgs {
+  HeadsView qi, qo, ki, ko;      // ki.heads == 0: no K
+  const double* freq;
+  const int32_t* pos;
+  int64_t pos_b;
+  int B, N, D, rot;
+  float magnitude;
+  bool f32, half, backward, vec; // vec: every access can be 16 bytes
+  bool copy;                     // channels from rot on have to be copied
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+
+// cache_rw.hip
+enum CacheFormat { kCacheBf16 = 0, kCacheE4m3 = 1, kCacheInt8 = 2 };
+
+struct CacheView {
+  void* k;
+  void* v;
+  float* ks;
+  float* vs;
+  int format, num_pages, heads, log2_page, D;
+};
+struct CacheRowsArgs {
+  CacheView c;
+  HeadsView k, v;
+  const int32_t* slots;
+  int64_t slots_b;
+  int B, N;
+  bool f32;
+};
+hipError_t launch_cache_write(const CacheRowsArgs& a, hipStream_t stream);
+hipError_t launch_cache_read(const CacheRowsArgs& a, hipStream_t stream);
+
+// cache_attention.hip
+struct CacheAttnArgs {
+  CacheView c;
+  HeadsView q, kn, vn, out;      // kn.p null: no drafted keys
+  const int32_t* table;
+  const int32_t* lens;
+  const uint8_t* mask;           // null: causal
+  int64_t mask_b;
+  const int32_t* counts;
+  float* ws;
+  float* lse;
+  int B, H, G, T, max_pages;     // G = H / kv heads
+  float scale_log2;
+  bool out_f32;
+};
+// Workgroups and 16-row tiles of a call, and its workspace.
+struct CacheAttnShape {
+  int qt;                        // 16-row tiles of a workgroup (1, 2 or 4)
+  int wgs;                       // workgroups
+  bool split;                    // whether a sequence's keys may be divided
+  size_t ws_bytes;
+};
+CacheAttnShape cache_attn_shape(const CacheAttnArgs& a);
+hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream);
+
+}  // namespace sva

@@ -1,0 +1,54 @@
+// How the keys of a call are divided among workgroups (cache_attn_kernel.h,
+// cache_attention.hip).  Host and device code, so that the division can be
+// checked without a GPU.
+//
+// A segment is one (batch entry, cache head, row tile); its keys are cut into
+// units of 128 (a 32-key step of each of four waves): first the cached keys,
+// then the drafted ones, at least one unit.  The units of all segments, in the
+// order (entry, head, tile, key), are dealt to n workgroups in runs of equal
+// length: workgroup i takes units i*U/n .. (i+1)*U/n - 1 of U.  However ragged the
+// lengths, every workgroup then reads the same number of keys; a run may cross
+// segments, and a segment whose units went to several workgroups is joined from
+// their partial results afterwards.  A workgroup leaves at most two of these:
+// slot 2i for a run that begins inside a segment, 2i + 1 for one that begins with a
+// segment and ends inside it.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sva {
+namespace cattn {
+
+constexpr int kUnit = 128;       // keys of a unit
+constexpr int kWaves = 4;
+
+struct Entry {                   // one batch entry
+  int len;                       // cached tokens
+  int cnt;                       // drafted tokens
+  int cached_units, units;       // of each of its segments
+  int tiles;                     // row tiles
+};
+
+__host__ __device__ __forceinline__ Entry entry_of(int len, int cnt, int max_len, int T, int G, int rows, bool drafts) {
+  Entry e;
+  e.len = len < 0 ? 0 : (len > max_len ? max_len : len);
+  e.cnt = cnt < 0 ? 0 : (cnt > T ? T : cnt);
+  e.cached_units = (int)(((int64_t)e.len + kUnit - 1) / kUnit);
+  e.units = e.cached_units + (drafts ? (e.cnt + kUnit - 1) / kUnit : 0);
+  if (e.units < 1) e.units = 1;
+  e.tiles = (int)(((int64_t)e.cnt * G + rows - 1) / rows);
+  return e;
+}
+
+// units of all of an entry's segments
+__host__ __device__ __forceinline__ int64_t entry_work(const Entry& e, int kv_heads) {
+  return (int64_t)e.units * e.tiles * kv_heads;
+}
+
+// first unit of workgroup i of n, of U units in all; the workgroup that has unit x
+__host__ __device__ __forceinline__ int64_t first_unit(int i, int n, int64_t U) { return U * i / n; }
+__host__ __device__ __forceinline__ int owner(int64_t x, int n, int64_t U) { return (int)(((x + 1) * n - 1) / U); }
+
+}  // namespace cattn
+}  // namespace sva

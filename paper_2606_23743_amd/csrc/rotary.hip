@@ -1,0 +1,222 @@
+// Rotary positions of Q and K: pair (a, b) number i of a row at position p
+// becomes m (a cos t - b sin t, a sin t + b cos t), t = p f_i (backward: -p f_i,
+// the transposed map).  Half layout: pair i is (x[i], x[i + rot/2]);
+// interleaved: (x[2i], x[2i + 1]).  Channels from rot on are copied, or left
+// alone in place.
+//
+// Bound by HBM: an element is read and written once and costs two products.
+// One workgroup takes a few tokens with all heads of Q and K, because a pair's
+// angle is the same in every head: it first tabulates (m cos t, m sin t) of its
+// tokens in LDS (the angle reduced modulo one turn in float64, so that positions
+// of a million are as exact as small ones), then streams rows, 16 bytes an
+// access, four items of a lane in flight.
+#include "sva_internal.h"
+
+namespace sva {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTab = 2048;       // (cos, sin) entries of a workgroup
+constexpr int kMaxTok = 16;      // tokens of a workgroup
+constexpr int kUnroll = 4;
+
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+struct RotaryGrid {
+  int tok;                       // tokens of a workgroup
+  int rot_items, row_items;      // items of a row that turn, and all of them
+};
+
+template <bool F32> struct Elem;
+template <> struct Elem<false> {
+  typedef uint16_t T;
+  static __device__ __forceinline__ float get(T x) { return __uint_as_float((uint32_t)x << 16); }
+  static __device__ __forceinline__ T put(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+  // 16 bytes as 8 floats and back
+  static constexpr int E = 8;
+  static __device__ __forceinline__ void wide(const u32x4& w, float (&y)[E]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[2 * i] = __uint_as_float(w[i] << 16);
+      y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ u32x4 narrow(const float (&y)[E]) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x2 f = {y[2 * i], y[2 * i + 1]};
+      w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));   // nearest, ties to even
+    }
+    return w;
+  }
+};
+template <> struct Elem<true> {
+  typedef float T;
+  static __device__ __forceinline__ float get(T x) { return x; }
+  static __device__ __forceinline__ T put(float x) { return x; }
+  static constexpr int E = 4;
+  static __device__ __forceinline__ void wide(const u32x4& w, float (&y)[E]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(w[i]);
+  }
+  static __device__ __forceinline__ u32x4 narrow(const float (&y)[E]) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(y[i]);
+    return w;
+  }
+};
+
+template <bool F32, bool HALF, bool VEC>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGrid gr) {
+  using El = Elem<F32>;
+  using T = typename El::T;
+  constexpr int E = VEC ? El::E : 1;
+  __shared__ float2 tab[kTab];
+  __shared__ int64_t base[kMaxTok][4];         // offsets of a token in q_in, q_out, k_in, k_out
+
+  const int np = a.rot / 2;
+  const int t0 = blockIdx.x * gr.tok;
+  const int nt = min(gr.tok, a.B * a.N - t0);
+  if (threadIdx.x < nt) {
+    const int b = (t0 + threadIdx.x) / a.N;
+    const int64_t n = t0 + threadIdx.x - b * a.N;
+    base[threadIdx.x][0] = b * a.qi.sb + n * a.qi.sn;
+    base[threadIdx.x][1] = b * a.qo.sb + n * a.qo.sn;
+    base[threadIdx.x][2] = b * a.ki.sb + n * a.ki.sn;
+    base[threadIdx.x][3] = b * a.ko.sb + n * a.ko.sn;
+  }
+  for (int e = threadIdx.x; e < nt * np; e += kThreads) {
+    const int tk = e / np, p = e - tk * np;
+    const int b = (t0 + tk) / a.N, n = t0 + tk - b * a.N;
+    double turn = (double)a.pos[b * a.pos_b + n] * (a.freq[p] * 0.15915494309189533576888);   // 1 / 2pi
+    turn -= rint(turn);
+    float sn, cs;
+    sincospif(2.0f * (float)turn, &sn, &cs);
+    tab[e] = make_float2(cs * a.magnitude, (a.backward ? -sn : sn) * a.magnitude);
+  }
+  __syncthreads();
+
+  const int heads = a.qi.heads + a.ki.heads;
+  const int items = nt * heads * gr.row_items;
+  for (int i0 = 0; i0 < items; i0 += kThreads * kUnroll) {
+    const T* src[kUnroll];
+    T* dst[kUnroll];
+    const float2* cs[kUnroll];
+    int c[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      // lanes past the end load the last item and store nothing
+      const unsigned idx = min(i0 + u * kThreads + (int)threadIdx.x, items - 1);
+      const unsigned row = idx / (unsigned)gr.row_items;
+      c[u] = idx - row * gr.row_items;
+      const unsigned tk = row / (unsigned)heads;
+      const int h = row - tk * heads;
+      const bool isq = h < a.qi.heads;
+      const int hh = isq ? h : h - a.qi.heads;
+      src[u] = (const T*)(isq ? a.qi.p : a.ki.p) + base[tk][isq ? 0 : 2] + hh * (isq ? a.qi.sh : a.ki.sh);
+      dst[u] = (T*)(isq ? a.qo.p : a.ko.p) + base[tk][isq ? 1 : 3] + hh * (isq ? a.qo.sh : a.ko.sh);
+      cs[u] = tab + tk * np;
+    }
+    auto live = [&](int u) { return i0 + u * kThreads + (int)threadIdx.x < items; };
+    if constexpr (VEC) {
+      u32x4 w[kUnroll][2];
+      int at[kUnroll][2];                      // first channels of an item's one or two pieces
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const bool turns = c[u] < gr.rot_items;
+        at[u][0] = turns ? c[u] * E : a.rot + (c[u] - gr.rot_items) * E;
+        at[u][1] = HALF && turns ? at[u][0] + np : at[u][0];
+        w[u][0] = *reinterpret_cast<const u32x4*>(src[u] + at[u][0]);
+        if constexpr (HALF) w[u][1] = *reinterpret_cast<const u32x4*>(src[u] + at[u][1]);
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (!live(u)) continue;
+        if (c[u] < gr.rot_items) {
+          float y[E], z[E];
+          El::wide(w[u][0], y);
+          if constexpr (HALF) {
+            El::wide(w[u][1], z);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const float2 t = cs[u][c[u] * E + e];
+              const float p = y[e], q = z[e];
+              y[e] = p * t.x - q * t.y;
+              z[e] = p * t.y + q * t.x;
+            }
+            *reinterpret_cast<u32x4*>(dst[u] + at[u][1]) = El::narrow(z);
+          } else {
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) {
+              const float2 t = cs[u][c[u] * (E / 2) + e];
+              const float p = y[2 * e], q = y[2 * e + 1];
+              y[2 * e] = p * t.x - q * t.y;
+              y[2 * e + 1] = p * t.y + q * t.x;
+            }
+          }
+          w[u][0] = El::narrow(y);
+        } else if (src[u] == dst[u]) {
+          continue;                            // in place: nothing to copy
+        }
+        *reinterpret_cast<u32x4*>(dst[u] + at[u][0]) = w[u][0];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (!live(u)) continue;
+        if (c[u] < gr.rot_items) {             // one pair
+          const int i = HALF ? c[u] : 2 * c[u], j = HALF ? c[u] + np : 2 * c[u] + 1;
+          const float2 t = cs[u][c[u]];
+          const float p = El::get(src[u][i]), q = El::get(src[u][j]);
+          dst[u][i] = El::put(p * t.x - q * t.y);
+          dst[u][j] = El::put(p * t.y + q * t.x);
+        } else {
+          const int i = a.rot + c[u] - gr.rot_items;
+          dst[u][i] = src[u][i];
+        }
+      }
+    }
+  }
+}
+
+template <bool F32, bool HALF, bool VEC>
+void launch_as(const RotaryArgs& a, hipStream_t stream) {
+  constexpr int E = VEC ? Elem<F32>::E : 1;
+  RotaryGrid gr;
+  gr.rot_items = !VEC || HALF ? a.rot / 2 / E : a.rot / E;
+  gr.row_items = gr.rot_items + (a.copy ? (a.D - a.rot) / E : 0);
+  // about four items a lane, within the table
+  const int64_t per_token = (int64_t)(a.qi.heads + a.ki.heads) * gr.row_items;
+  int64_t tok = kThreads * kUnroll / (per_token > 0 ? per_token : 1);
+  tok = tok < 1 ? 1 : (tok > kMaxTok ? kMaxTok : tok);
+  if (tok > kTab / (a.rot / 2)) tok = kTab / (a.rot / 2);
+  gr.tok = (int)tok;
+  const int64_t tokens = (int64_t)a.B * a.N;
+  hipLaunchKernelGGL((rotary_kernel<F32, HALF, VEC>), dim3((unsigned)((tokens + tok - 1) / tok)), dim3(kThreads), 0,
+                     stream, a, gr);
+}
+
+template <bool F32, bool HALF>
+void launch_layout(const RotaryArgs& a, hipStream_t stream) {
+  if (a.vec) launch_as<F32, HALF, true>(a, stream);
+  else launch_as<F32, HALF, false>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream) {
+  if (a.f32) {
+    if (a.half) launch_layout<true, true>(a, stream);
+    else launch_layout<true, false>(a, stream);
+  } else {
+    if (a.half) launch_layout<false, true>(a, stream);
+    else launch_layout<false, false>(a, stream);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace sva

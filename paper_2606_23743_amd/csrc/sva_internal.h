@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "attn_args.h"
+#include "cache_args.h"
 #include "xcd.h"
 
 namespace sva {
