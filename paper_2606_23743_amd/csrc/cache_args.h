@@ -62,14 +62,19 @@ struct CacheAttnArgs {
   float scale_log2;
   bool out_f32;
 };
-// Workgroups and 16-row tiles of a call, and its workspace.
+// How a call is run, and its workspace.
 struct CacheAttnShape {
-  int qt;                        // 16-row tiles of a workgroup (1, 2 or 4)
+  bool shared;                   // waves share their keys (cache_attn_tile.h), or each has its own
+  int tiles;                     // 16-row tiles of a workgroup: 1 or 2; shared: 4 or 8
   int wgs;                       // workgroups
   bool split;                    // whether a sequence's keys may be divided
   size_t ws_bytes;
 };
 CacheAttnShape cache_attn_shape(const CacheAttnArgs& a);
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream);
+// one cache format each
+hipError_t launch_cache_attention_bf16(const CacheAttnArgs& a, const CacheAttnShape& s, hipStream_t stream);
+hipError_t launch_cache_attention_e4m3(const CacheAttnArgs& a, const CacheAttnShape& s, hipStream_t stream);
+hipError_t launch_cache_attention_int8(const CacheAttnArgs& a, const CacheAttnShape& s, hipStream_t stream);
 
 }  // namespace sva

@@ -1,53 +1,160 @@
-// Dispatch of the attention over a paged cache, and the join of divided segments.
-#include "cache_attn_kernel.h"
+// Shape and dispatch of the attention over a paged cache, and the join of divided
+// segments.
+#include "cache_attn_common.h"
 
 namespace sva {
-
+namespace cattn {
 namespace {
 
-constexpr int kCus = 256;
+// The partial results of one 16-row tile's channels (one of the four that a lane
+// row splits into) of a divided segment, joined in the order of the workgroups.
+constexpr int kJoinGroups = 4;
 
 template <int D>
-void launch_join(const CacheAttnArgs& a, const CacheAttnShape& s, int tiles, hipStream_t stream) {
-  using namespace cattn;
-  const dim3 grid((unsigned)((int64_t)a.B * a.c.heads * tiles * s.qt * kWaves));
-  const dim3 block(64 * kJoinGroups);
-  if (s.qt == 1) hipLaunchKernelGGL((cache_join_kernel<D, 1>), grid, block, 0, stream, a, s.wgs, tiles);
-  else if (s.qt == 2) hipLaunchKernelGGL((cache_join_kernel<D, 2>), grid, block, 0, stream, a, s.wgs, tiles);
-  else hipLaunchKernelGGL((cache_join_kernel<D, 4>), grid, block, 0, stream, a, s.wgs, tiles);
+__global__ __launch_bounds__(64 * kJoinGroups) void cache_join_kernel(CacheAttnArgs a, int grid_n, int nt, int max_tiles) {
+  using PT = Part<D>;
+  constexpr int JT = PT::JT;
+  const int RPT = 16 * nt;                         // rows of a segment
+  __shared__ __attribute__((aligned(16))) float so[kJoinGroups][64][JT];
+  __shared__ float sm[kJoinGroups][16], sl[kJoinGroups][16];
+  const int lane = threadIdx.x & 63, g = lane >> 4, i16 = lane & 15;
+  const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int id = blockIdx.x;
+  const int w = id % kWaves;
+  id /= kWaves;
+  const int qt = id % nt;
+  id /= nt;
+  const int rt = id % max_tiles;
+  id /= max_tiles;
+  const int h = id % a.c.heads, b = id / a.c.heads;
+
+  const Finder fd(a, RPT);
+  const Entry en = fd.at(b);
+  if (rt >= en.tiles || (rt * RPT + qt * 16) >= en.cnt * a.G) return;
+  const int64_t U = fd.total;
+  const int n = (int)min((int64_t)grid_n, U);
+  // the entry's first unit: the scan up to b
+  int64_t base = 0;
+  for (int b0 = 0; b0 < b; b0 += 64) {
+    const int64_t in = a.B <= 64 ? fd.incl : fd.scan(b0);
+    base += uniform(__shfl(in, min(b - b0, 64) - 1));
+  }
+  const int64_t s0 = base + ((int64_t)h * en.tiles + rt) * en.units;
+  const int i0 = uniform(owner(s0, n, U)), i1 = uniform(owner(s0 + en.units - 1, n, U));
+  if (i0 == i1) return;                            // one workgroup had it all, and wrote it
+
+  auto slot = [&](int i) { return 2 * i + (i == i0 ? 1 : 0); };   // i0's run holds the segment's first unit
+  float m = -INFINITY, l = 0.0f;
+  float y[JT] = {};
+  constexpr int UN = 4;
+  for (int k0 = i0 + grp; k0 <= i1; k0 += kJoinGroups * UN) {
+    float4 p[UN][JT / 4];
+    float pm[UN], pl[UN];
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      const int i = min(k0 + k * kJoinGroups, i1);
+      const float* part = a.ws + (int64_t)slot(i) * PT::floats(nt);
+      const float* from = part + PT::at(qt, w, lane);
+#pragma unroll
+      for (int j = 0; j < JT / 4; ++j) p[k][j] = *reinterpret_cast<const float4*>(from + 4 * j);
+      pm[k] = part[PT::ref(nt, qt * 16 + i16)];
+      pl[k] = part[PT::sum(nt, qt * 16 + i16)];
+    }
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      if (k0 + k * kJoinGroups > i1) break;
+      const float to = fmaxf(m, pm[k]);
+      const float ref = to == -INFINITY ? 0.0f : to;
+      const float f0 = __builtin_amdgcn_exp2f(m - ref), f1 = __builtin_amdgcn_exp2f(pm[k] - ref);
+      m = to;
+      l = l * f0 + pl[k] * f1;
+#pragma unroll
+      for (int j = 0; j < JT / 4; ++j) {
+        y[4 * j] = y[4 * j] * f0 + p[k][j].x * f1;
+        y[4 * j + 1] = y[4 * j + 1] * f0 + p[k][j].y * f1;
+        y[4 * j + 2] = y[4 * j + 2] * f0 + p[k][j].z * f1;
+        y[4 * j + 3] = y[4 * j + 3] * f0 + p[k][j].w * f1;
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < JT; ++j) so[grp][lane][j] = y[j];
+  if (g == 0) {
+    sm[grp][i16] = m;
+    sl[grp][i16] = l;
+  }
+  __syncthreads();
+  if (grp != 0) return;
+  float top = sm[0][i16];
+#pragma unroll
+  for (int k = 1; k < kJoinGroups; ++k) top = fmaxf(top, sm[k][i16]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  l = 0.0f;
+#pragma unroll
+  for (int j = 0; j < JT; ++j) y[j] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kJoinGroups; ++k) {
+    const float f = __builtin_amdgcn_exp2f(sm[k][i16] - ref);
+    l += sl[k][i16] * f;
+#pragma unroll
+    for (int j = 0; j < JT; ++j) y[j] += so[k][lane][j] * f;
+  }
+  const int row = rt * RPT + qt * 16 + i16;
+  const int t = row / a.G, head = h * a.G + (row - t * a.G);
+  if (t >= en.cnt) return;
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int j = 0; j < JT; ++j) y[j] = l == 0.0f ? 0.0f : y[j] * inv;
+  const int d0 = JT * (4 * g + w);
+  if (d0 < D) store_row<D>(a, b, head, t, d0, y);
+  if (a.lse && w == 0 && g == 0)
+    a.lse[((int64_t)b * a.H + head) * a.T + t] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
+}
+
+template <int D>
+void launch_join(const CacheAttnArgs& a, const CacheAttnShape& s, hipStream_t stream) {
+  const int segments = (int)(((int64_t)a.G * a.T + 16 * s.tiles - 1) / (16 * s.tiles));
+  const dim3 grid((unsigned)((int64_t)a.B * a.c.heads * segments * s.tiles * kWaves));
+  hipLaunchKernelGGL(cache_join_kernel<D>, grid, dim3(64 * kJoinGroups), 0, stream, a, s.wgs, s.tiles, segments);
 }
 
 }  // namespace
+}  // namespace cattn
 
 CacheAttnShape cache_attn_shape(const CacheAttnArgs& a) {
   using namespace cattn;
+  constexpr int kCus = 256;
   CacheAttnShape s{};
   const int64_t rows = (int64_t)a.G * a.T;
-  s.qt = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
+  s.shared = rows > 16;
+  s.tiles = 1;
+  if (s.shared) {
+    const int64_t passes = (rows + 127) / 128;     // 128 rows are what a workgroup's registers hold
+    s.tiles = 4 * (int)(((rows + passes - 1) / passes + 63) / 64);
+  }
   // as many workgroups as are resident at once
-  const int resident = kCus * (s.qt == 1 ? 4 : 2);
-  const Entry e = entry_of(a.max_pages << a.c.log2_page, a.T, a.max_pages << a.c.log2_page, a.T, a.G, 16 * s.qt, true);
+  const int resident = kCus * 2;
+  const int cap = a.max_pages << a.c.log2_page;
+  const Entry e = entry_of(cap, a.T, cap, a.T, a.G, 16 * s.tiles, true);
   const int64_t most = entry_work(e, a.c.heads) * a.B;
   s.wgs = (int)(most < resident ? most : resident);
   s.split = e.units > 1;
-  const int64_t floats = (int64_t)16 * s.qt * ((a.c.D > 64 ? 128 : 64) + 2);
-  s.ws_bytes = s.split ? (size_t)(2 * s.wgs * floats * 4) : 0;
+  const size_t floats = a.c.D > 64 ? Part<128>::floats(s.tiles) : Part<64>::floats(s.tiles);
+  s.ws_bytes = s.split ? (size_t)2 * s.wgs * floats * 4 : 0;
   return s;
 }
 
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream) {
-  using namespace cattn;
   const CacheAttnShape s = cache_attn_shape(a);
   hipError_t e;
-  if (a.c.format == kCacheBf16) e = launch_bf16(a, s, stream);
-  else if (a.c.format == kCacheE4m3) e = launch_e4m3(a, s, stream);
-  else e = launch_int8(a, s, stream);
+  if (a.c.format == kCacheBf16) e = launch_cache_attention_bf16(a, s, stream);
+  else if (a.c.format == kCacheE4m3) e = launch_cache_attention_e4m3(a, s, stream);
+  else e = launch_cache_attention_int8(a, s, stream);
   if (e != hipSuccess || !s.split) return e;
-  const int tiles = (int)(((int64_t)a.G * a.T + 16 * s.qt - 1) / (16 * s.qt));
   switch (a.c.D) {
-    case 64: launch_join<64>(a, s, tiles, stream); break;
-    case 112: launch_join<112>(a, s, tiles, stream); break;
-    default: launch_join<128>(a, s, tiles, stream); break;
+    case 64: cattn::launch_join<64>(a, s, stream); break;
+    case 112: cattn::launch_join<112>(a, s, stream); break;
+    default: cattn::launch_join<128>(a, s, stream); break;
   }
   return hipGetLastError();
 }

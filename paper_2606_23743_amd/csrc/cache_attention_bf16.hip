@@ -1,12 +1,10 @@
-// cache_attn_kernel.h over a bf16 cache.
-#include "cache_attn_kernel.h"
+// The attention over a paged bf16 cache (cache_attn_kernel.h, cache_attn_tile.h).
+#include "cache_attn_dispatch.h"
 
 namespace sva {
-namespace cattn {
 
-hipError_t launch_bf16(const CacheAttnArgs& a, const CacheAttnShape& s, hipStream_t stream) {
-  return launch_format<kCacheBf16>(a, s, stream);
+hipError_t launch_cache_attention_bf16(const CacheAttnArgs& a, const CacheAttnShape& s, hipStream_t stream) {
+  return cattn::launch_format<kCacheBf16>(a, s, stream);
 }
 
-}  // namespace cattn
 }  // namespace sva

@@ -1,0 +1,148 @@
+// What the kernels of the attention over a paged cache share (cache_attn_kernel.h,
+// cache_attn_tile.h, cache_attention.hip).
+#pragma once
+
+#include "attn_w16.h"
+#include "cache_attn_plan.h"
+
+namespace sva {
+namespace cattn {
+
+using attn::bf16x2;
+using attn::bf16x8;
+using attn::f32x2;
+using attn::f32x4;
+using attn::u32x2;
+using attn::u32x4;
+
+// four codes (bytes) -> four bf16 values in two dwords
+template <int FMT>
+__device__ __forceinline__ u32x2 widen4(uint32_t c) {
+  u32x2 o;
+  if constexpr (FMT == kCacheE4m3) {
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, true));
+  } else {
+    // whole numbers up to 127 in float32: the upper halves are their bf16 values
+    const float a = (float)((int)(c << 24) >> 24), b = (float)((int)(c << 16) >> 24);
+    const float d = (float)((int)(c << 8) >> 24), e = (float)((int)c >> 24);
+    o[0] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    o[1] = __builtin_amdgcn_perm(__float_as_uint(e), __float_as_uint(d), 0x07060302u);
+  }
+  return o;
+}
+
+// weights times V scales as NP B operands: rounded to bf16 (NP = 1, bf16 results), or as
+// the sum of three bf16 values, which holds all 24 bits (float32 results: with two
+// parts they were off by 1.4e-6 of their norm, with three by what the logits are)
+template <int QT, int NP>
+__device__ __forceinline__ void weight_operands(const float (&p)[QT][8], bf16x8 (&part)[NP][QT]) {
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    float a[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = p[qt][e];
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      u32x4 h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        h[e] = __builtin_bit_cast(uint32_t, attn::cvt2(a[2 * e], a[2 * e + 1]));
+        a[2 * e] -= __uint_as_float(h[e] << 16);
+        a[2 * e + 1] -= __uint_as_float(h[e] & 0xFFFF0000u);
+      }
+      part[n][qt] = __builtin_bit_cast(bf16x8, h);
+    }
+  }
+}
+
+// values that every lane holds alike, as scalars
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// units of all segments, and the entry that unit x falls into with its first unit; by one wave
+struct Finder {
+  const CacheAttnArgs& a;
+  int rows;
+  int64_t incl;                  // B <= 64: the scan of the only chunk
+  int64_t total;
+
+  __device__ __forceinline__ Entry of(int len, int cnt) const {
+    return entry_of(len, cnt, a.max_pages << a.c.log2_page, a.T, a.G, rows, a.kn.p != nullptr);
+  }
+  // b alike in all lanes
+  __device__ __forceinline__ Entry at(int b) const {
+    return of(uniform(a.lens[b]), a.counts ? uniform(a.counts[b]) : a.T);
+  }
+  __device__ __forceinline__ int64_t scan(int b0) const {
+    const int b = b0 + (int)(threadIdx.x & 63);
+    int64_t x = b < a.B ? entry_work(of(a.lens[b], a.counts ? a.counts[b] : a.T), a.c.heads) : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t y = __shfl_up(x, d);
+      if ((int)(threadIdx.x & 63) >= d) x += y;
+    }
+    return x;
+  }
+  __device__ __forceinline__ Finder(const CacheAttnArgs& args, int rows_) : a(args), rows(rows_) {
+    total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      incl = scan(b0);
+      total += uniform(__shfl(incl, 63));
+    }
+  }
+  // x < total
+  __device__ __forceinline__ int find(int64_t x, int64_t& first) const {
+    int64_t base = 0;
+    for (int b0 = 0;; b0 += 64) {
+      const int64_t in = a.B <= 64 ? incl : scan(b0);
+      const uint64_t past = __builtin_amdgcn_ballot_w64(base + in > x);
+      if (past != 0) {
+        const int k = __builtin_ctzll(past);
+        first = base + (k > 0 ? uniform(__shfl(in, k > 0 ? k - 1 : 0)) : 0);
+        return b0 + k;
+      }
+      base += uniform(__shfl(in, 63));
+    }
+  }
+};
+
+// A partial result in the workspace: for each 16-row tile, 4 x 64 x JT floats in the
+// order of the join's lanes (channels JT * (4g + w) .. + JT - 1 of row i at [w][16g + i]),
+// then every row's reference, then every row's sum.
+template <int D>
+struct Part {
+  static constexpr int JT = D > 64 ? 8 : 4;
+  static constexpr int kTile = kWaves * 64 * JT;
+  static __host__ __device__ constexpr int floats(int tiles) { return tiles * (kTile + 32); }
+  static __device__ __forceinline__ int at(int tile, int w, int lane) { return tile * kTile + (w * 64 + lane) * JT; }
+  static __device__ __forceinline__ int ref(int tiles, int row) { return tiles * kTile + row; }
+  static __device__ __forceinline__ int sum(int tiles, int row) { return tiles * (kTile + 16) + row; }
+};
+
+template <int D>
+__device__ __forceinline__ void store_row(const CacheAttnArgs& a, int b, int h, int t, int d0,
+                                          const float* y) {
+  constexpr int JT = D > 64 ? 8 : 4;
+  const int64_t at = b * a.out.sb + h * a.out.sh + t * a.out.sn + d0;
+  if (a.out_f32) {
+    float* o = static_cast<float*>(a.out.p) + at;
+#pragma unroll
+    for (int e = 0; e < JT; e += 4) *reinterpret_cast<float4*>(o + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+  } else {
+    uint16_t* o = static_cast<uint16_t*>(a.out.p) + at;
+    uint32_t w[JT / 2];
+#pragma unroll
+    for (int e = 0; e < JT / 2; ++e) w[e] = __builtin_bit_cast(uint32_t, attn::cvt2(y[2 * e], y[2 * e + 1]));
+    if constexpr (JT == 8) *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
+  }
+}
+
+constexpr float kLn2 = 0.69314718055994530942f;
+
+}  // namespace cattn
+}  // namespace sva

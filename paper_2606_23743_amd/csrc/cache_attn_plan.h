@@ -46,9 +46,19 @@ __host__ __device__ __forceinline__ int64_t entry_work(const Entry& e, int kv_he
   return (int64_t)e.units * e.tiles * kv_heads;
 }
 
+// floor(a / b) for 0 <= a < 2^52, b > 0, by a float64 quotient that is at most one off (a
+// 64-bit integer division is a hundred and fifty instructions here)
+__host__ __device__ __forceinline__ int64_t div_floor(int64_t a, int64_t b) {
+  int64_t q = (int64_t)((double)a / (double)b);
+  const int64_t r = a - q * b;
+  if (r < 0) --q;
+  if (r >= b) ++q;
+  return q;
+}
+
 // first unit of workgroup i of n, of U units in all; the workgroup that has unit x
-__host__ __device__ __forceinline__ int64_t first_unit(int i, int n, int64_t U) { return U * i / n; }
-__host__ __device__ __forceinline__ int owner(int64_t x, int n, int64_t U) { return (int)(((x + 1) * n - 1) / U); }
+__host__ __device__ __forceinline__ int64_t first_unit(int i, int n, int64_t U) { return div_floor(U * i, n); }
+__host__ __device__ __forceinline__ int owner(int64_t x, int n, int64_t U) { return (int)div_floor((x + 1) * n - 1, U); }
 
 }  // namespace cattn
 }  // namespace sva
