@@ -65,7 +65,7 @@ struct CacheAttnArgs {
 // How a call is run, and its workspace.
 struct CacheAttnShape {
   bool shared;                   // waves share their keys (cache_attn_tile.h), or each has its own
-  int tiles;                     // 16-row tiles of a workgroup: 1 or 2; shared: 4 or 8
+  int tiles;                     // 16-row tiles of a workgroup: 1 to 3; shared: 4 or 8
   int wgs;                       // workgroups
   bool split;                    // whether a sequence's keys may be divided
   size_t ws_bytes;

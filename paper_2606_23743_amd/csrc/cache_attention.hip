@@ -126,14 +126,20 @@ CacheAttnShape cache_attn_shape(const CacheAttnArgs& a) {
   constexpr int kCus = 256;
   CacheAttnShape s{};
   const int64_t rows = (int64_t)a.G * a.T;
-  s.shared = rows > 16;
-  s.tiles = 1;
+  // Up to three 16-row tiles each wave holds the state of all rows and has keys of its
+  // own; past that the registers do not, and the waves share keys and divide rows.  us at
+  // two sequences of 223,200 and 8 cache heads, 30 / 48 rows: own keys 165 / 194 (e4m3),
+  // 285 / 310 (bf16); shared 277 / 282, 303 / 345.  At 192 rows of 8 int8 sequences 185 (in
+  // four passes over the keys) against 163.
+  s.shared = rows > 48;
   if (s.shared) {
     const int64_t passes = (rows + 127) / 128;     // 128 rows are what a workgroup's registers hold
     s.tiles = 4 * (int)(((rows + passes - 1) / passes + 63) / 64);
+  } else {
+    s.tiles = (int)((rows + 15) / 16);
   }
   // as many workgroups as are resident at once
-  const int resident = kCus * 2;
+  const int resident = kCus * (s.shared ? 2 : wave_residents(a.c.D, s.tiles));
   const int cap = a.max_pages << a.c.log2_page;
   const Entry e = entry_of(cap, a.T, cap, a.T, a.G, 16 * s.tiles, true);
   const int64_t most = entry_work(e, a.c.heads) * a.B;

@@ -13,7 +13,9 @@ void launch_dim(const CacheAttnArgs& a, const CacheAttnShape& s, hipStream_t str
     if (s.tiles == 4) launch_tile<FMT, D, 1>(a, s.wgs, stream);
     else launch_tile<FMT, D, 2>(a, s.wgs, stream);
   } else {
-    launch_wave<FMT, D, 1>(a, s.wgs, stream);
+    if (s.tiles == 1) launch_wave<FMT, D, 1>(a, s.wgs, stream);
+    else if (s.tiles == 2) launch_wave<FMT, D, 2>(a, s.wgs, stream);
+    else launch_wave<FMT, D, 3>(a, s.wgs, stream);
   }
 }
 

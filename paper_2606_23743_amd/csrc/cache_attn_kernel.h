@@ -56,8 +56,13 @@ struct Raw {
   u32x4 k[2][G::NPK];
   uint32_t v[8][G::NW];
   f32x4 ks[2], vs[2];            // 8 bits: scales of the lane's eight keys
+  int64_t row;                   // the first of them in the cache
   bool there;                    // their page exists
 };
+
+// codes are read once: past the caches
+template <class T>
+__device__ __forceinline__ T stream(const T* p) { return __builtin_nontemporal_load(p); }
 
 // V^T operand of tile j: channel JT * r + j of keys 8g .. 8g + 7.  8-bit codes are
 // transposed four channels at a time (t: the bytes of keys 0..3 and 4..7 of each).
@@ -84,11 +89,12 @@ __device__ __forceinline__ void transpose8(const uint32_t (&v)[8][NW], int w, ui
 }
 
 // one wave's running state for QT tiles of 16 rows
-template <int D, int QT>
+template <int D, int QT, int NP>
 struct State {
   static constexpr int JT = D > 64 ? 8 : 4;
   f32x4 o[JT][QT];
   float m[QT], l[QT];            // reference (base 2) of the lane's column; the lane's part of the sum
+  bf16x8 wp[NP][QT];             // the step's weights as B operands
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -100,62 +106,67 @@ struct State {
     }
   }
 
-  // logits (base 2, -inf where masked) -> weights in place; the reference moves up
-  // where a column passes it by 8
-  __device__ __forceinline__ void weigh(float (&s)[QT][8]) {
-    bool grow = false;
-    float top[QT];
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      top[qt] = s[qt][0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) top[qt] = fmaxf(top[qt], s[qt][e]);
-      grow |= top[qt] > m[qt] + 8.0f;
-    }
-    if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        const float to = fmaxf(m[qt], attn::quad_max(top[qt]));
-        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[qt] - to);
-        m[qt] = to;
-        l[qt] *= f;
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[j][qt][r] *= f;
-      }
-    }
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      const float ref = m[qt] == -INFINITY ? 0.0f : m[qt];   // only masked keys so far: weights of zero
-      float sum = 0.0f;
+  // logits s * f (base 2; s = -inf where masked) of one row tile -> weights, times z the
+  // operands of the product with V.  Weights are positive: where their sum stays below
+  // 2^10, each one does, and the reference stays where it is.
+  __device__ __forceinline__ void weigh(int qt, const f32x4 (&s)[2], const float (&f)[8], const float (&z)[8], bool scaled) {
+    float p[8], sum;
+    auto weights = [&](float ref) {
+      sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s[qt][e] = __builtin_amdgcn_exp2f(s[qt][e] - ref);
-        sum += s[qt][e];
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][e & 3], f[e], -ref));
+        sum += p[e];
       }
-      l[qt] += sum;
+    };
+    weights(m[qt]);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(sum > 1024.0f || m[qt] == -INFINITY) != 0, 0)) {
+      asm volatile("");                            // a branch that is rarely taken, not selects
+      float top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, s[e >> 2][e & 3] * f[e]);
+      const float to = fmaxf(m[qt], attn::quad_max(top));
+      const float ref = to == -INFINITY ? 0.0f : to;   // only masked keys so far: weights of zero
+      const float c = __builtin_amdgcn_exp2f(m[qt] - ref);
+      m[qt] = to;
+      l[qt] *= c;
+#pragma unroll
+      for (int j = 0; j < JT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[j][qt][r] *= c;
+      weights(ref);
     }
+    l[qt] += sum;
+    if (scaled) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] *= z[e];
+    }
+    float pp[1][8];
+    bf16x8 part[NP][1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pp[0][e] = p[e];
+    weight_operands<1, NP>(pp, part);
+#pragma unroll
+    for (int n = 0; n < NP; ++n) wp[n][qt] = part[n][0];
+  }
+
+  __device__ __forceinline__ void add(int j, bf16x8 v) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+        o[j][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, wp[n][qt], o[j][qt], 0, 0, 0);
   }
 };
 
-template <int D, int QT, int NP>
-__device__ __forceinline__ void pv_tile(State<D, QT>& st, int j, bf16x8 v, const bf16x8 (&part)[NP][QT]) {
-#pragma unroll
-  for (int n = 0; n < NP; ++n)
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt)
-      st.o[j][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, part[n][qt], st.o[j][qt], 0, 0, 0);
-}
-
 template <int FMT, int D, int QT, int NP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(wave_residents(D, QT))))
 void cache_attn_kernel(CacheAttnArgs a) {
   using G = CGeo<FMT, D>;
-  using S = State<D, QT>;
   using PT = Part<D>;
   constexpr int JT = G::JT, KS = G::KS, RPT = 16 * QT;
   __shared__ __attribute__((aligned(16))) float so[kWaves][4][64][JT];   // one 16-row tile of each wave
+  __shared__ __attribute__((aligned(16))) u32x4 qs[QT][KS][64];          // Q as the lanes' B operands
   __shared__ float sm[kWaves][RPT], sl[kWaves][RPT];
 
   const int lane = threadIdx.x & 63, g = lane >> 4, i16 = lane & 15;
@@ -191,30 +202,54 @@ void cache_attn_kernel(CacheAttnArgs a) {
     const int h = uniform(seg / en.tiles), rt = seg - h * en.tiles;
     x += u1 - u0;
 
+    // the token and head of the lane's column in tile qt; token -1: no such row
+    auto row_of = [&](int qt, int& tok, int& head) {
+      const int row = rt * RPT + qt * 16 + i16, t = row / a.G;
+      tok = t < en.cnt ? t : -1;
+      head = h * a.G + (row - t * a.G);
+    };
     // ---- Q of this tile's rows ----
-    bf16x8 q[QT][KS];
-    int tok[QT], head[QT];                         // of the lane's column; tok = -1: no such row
+    auto load_q = [&](int qt, int s) {
+      int t, head;
+      row_of(qt, t, head);
+      const int d = chan<G::W8>(s, g);
+      u32x4 y{};
+      if (t >= 0 && d < D)
+        y = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q.p) + b * a.q.sb + head * a.q.sh + t * a.q.sn + d);
+      return y;
+    };
+    bf16x8 q1[KS];                                 // one tile stays in registers, more lie in LDS
+    if constexpr (QT == 1) {
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      const int row = rt * RPT + qt * 16 + i16;
-      const int t = row / a.G;
-      tok[qt] = t < en.cnt ? t : -1;
-      head[qt] = h * a.G + (row - t * a.G);
-      const uint16_t* p = static_cast<const uint16_t*>(a.q.p) + b * a.q.sb + head[qt] * a.q.sh + t * a.q.sn;
+      for (int s = 0; s < KS; ++s) q1[s] = __builtin_bit_cast(bf16x8, load_q(0, s));
+    } else {
+#pragma unroll 1
+      for (int qt = w; qt < QT; qt += kWaves)
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int d = chan<G::W8>(s, g);
-        if (tok[qt] >= 0 && d < D) q[qt][s] = *reinterpret_cast<const bf16x8*>(p + d);
-        else q[qt][s] = bf16x8{};
-      }
+        for (int s = 0; s < KS; ++s) qs[qt][s][lane] = load_q(qt, s);
+      __syncthreads();
     }
+    auto q_operand = [&](int qt, int s) {
+      if constexpr (QT == 1) return q1[s];
+      return __builtin_bit_cast(bf16x8, qs[qt][s][lane]);
+    };
 
-    S st;
+    State<D, QT, NP> st;
     st.clear();
 
+    // logits of one row tile: K of 16 keys each in kw[t]
+    auto scores = [&](const u32x4 (&kw)[2][KS], int qt, f32x4 (&s)[2]) {
+      s[0] = s[1] = f32x4{};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const bf16x8 qv = q_operand(qt, k);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw[t][k]), qv, s[t], 0, 0, 0);
+      }
+    };
+
     // ---- cached keys ----
-    // A step's codes are loaded while the step before is worked on, and its page numbers
-    // before those loads, so that waiting for them waits for nothing else.
     const int32_t* table = a.table + (int64_t)b * a.max_pages;
     const int kq = 8 * (i16 >> 2), kv8 = 8 * g;    // this lane's K rows and V rows of a step begin here
     auto page_at = [&](int key) { return table[min(key >> log2p, a.max_pages - 1)]; };
@@ -226,41 +261,44 @@ void cache_attn_kernel(CacheAttnArgs a) {
       pk = page_at(u * kUnit + 32 * w + kq);
       pv = page_at(u * kUnit + 32 * w + kv8);
     };
-    auto load = [&](Raw<FMT, D>& r, int u) {       // with the pages loaded for it; then the next ones
+    // K and its scales, with the pages loaded for it; the next page numbers go out first, so
+    // that waiting for them waits for nothing else
+    auto load_k = [&](Raw<FMT, D>& r, int u) {
       const int key0 = u * kUnit + 32 * w;
       r.there = pv >= 0 && pv < a.c.num_pages;
       const int64_t gk = pk >= 0 && pk < a.c.num_pages ? pk : 0, gv = r.there ? pv : 0;
       const int64_t rk = ((gk * Hkv + h) << log2p) + ((key0 + kq) & pmask) + (i16 & 3);
-      const int64_t rv = ((gv * Hkv + h) << log2p) + ((key0 + kv8) & pmask);
+      r.row = ((gv * Hkv + h) << log2p) + ((key0 + kv8) & pmask);
       if (u + 1 < ulast) load_pages(u + 1);
       const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + rk * (D * G::EB);
-      const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + rv * (D * G::EB);
       // D = 112: groups past the row's end read its last piece, and drop it below
       auto piece = [&](int p) { return min(64 * p + 16 * g, D * G::EB - 16); };
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int p = 0; p < G::NPK; ++p)
-          r.k[t][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + t * 4 * D * G::EB + piece(p)));
+        for (int p = 0; p < G::NPK; ++p) r.k[t][p] = stream(reinterpret_cast<const u32x4*>(kp + t * 4 * D * G::EB + piece(p)));
       if constexpr (G::W8) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          r.ks[e] = *reinterpret_cast<const f32x4*>(a.c.ks + rv + 4 * e);
-          r.vs[e] = *reinterpret_cast<const f32x4*>(a.c.vs + rv + 4 * e);
-        }
+        for (int e = 0; e < 2; ++e) r.ks[e] = *reinterpret_cast<const f32x4*>(a.c.ks + r.row + 4 * e);
       }
-      const int vat = min(i16, G::VR - 1) * JT * G::EB;
+    };
+    auto load_v = [&](Raw<FMT, D>& r) {
+      if constexpr (G::W8) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) r.vs[e] = *reinterpret_cast<const f32x4*>(a.c.vs + r.row + 4 * e);
+      }
+      const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + r.row * (D * G::EB) + min(i16, G::VR - 1) * JT * G::EB;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint8_t* p = vp + e * D * G::EB + vat;
+        const uint8_t* p = vp + e * D * G::EB;
         if constexpr (G::NW == 1) {
-          r.v[e][0] = *reinterpret_cast<const uint32_t*>(p);
+          r.v[e][0] = stream(reinterpret_cast<const uint32_t*>(p));
         } else if constexpr (G::NW == 2) {
-          const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+          const u32x2 y = stream(reinterpret_cast<const u32x2*>(p));
           r.v[e][0] = y[0];
           r.v[e][1] = y[1];
         } else {
-          const u32x4 y = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+          const u32x4 y = stream(reinterpret_cast<const u32x4*>(p));
           r.v[e][0] = y[0];
           r.v[e][1] = y[1];
           r.v[e][2] = y[2];
@@ -268,65 +306,66 @@ void cache_attn_kernel(CacheAttnArgs a) {
         }
       }
     };
+    // One step.  K of the next one is loaded as soon as this one's is widened (bf16:
+    // multiplied) and V as soon as it is transposed: into the registers that this frees, so
+    // that a step's codes are on their way while the step before is worked on.  (Two sets in
+    // turn took 32 to 64 registers more; at D = 128 they were no faster in 8 bits, 137 us both for
+    // 840 MB, and spilled in bf16, 450 us for 279.)
     auto work_on = [&](Raw<FMT, D>& r, int u) {
-      const int key0 = u * kUnit + 32 * w;
-      f32x4 acc[2][QT];
+      const int left = en.len - u * kUnit - 32 * w;
+      const bool there = r.there, whole = left >= 32 && __builtin_amdgcn_ballot_w64(!there) == 0;
+      float f[8], z[8];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) acc[t][qt] = f32x4{};
+      for (int e = 0; e < 8; ++e) f[e] = G::W8 ? a.scale_log2 * r.ks[e >> 2][e & 3] : a.scale_log2;
+      u32x4 kw[2][KS];
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          // one operand at a time: widened all at once they would take 32 registers more
-          __builtin_amdgcn_sched_barrier(0);
-          u32x4 kw;
           if constexpr (G::W8) {
-            const u32x2 y = widen4<FMT>(r.k[t][s >> 1][2 * (s & 1)]), z = widen4<FMT>(r.k[t][s >> 1][2 * (s & 1) + 1]);
-            kw = u32x4{y[0], y[1], z[0], z[1]};
+            const u32x2 y = widen4<FMT>(r.k[t][s >> 1][2 * (s & 1)]), c = widen4<FMT>(r.k[t][s >> 1][2 * (s & 1) + 1]);
+            kw[t][s] = u32x4{y[0], y[1], c[0], c[1]};
           } else {
-            kw = r.k[t][s];
+            kw[t][s] = r.k[t][s];
           }
           if (D == 112 && chan<G::W8>(s, 3) >= D) {  // a step with absent channels
-            if (chan<G::W8>(s, g) >= D) kw = u32x4{};
+            if (chan<G::W8>(s, g) >= D) kw[t][s] = u32x4{};
           }
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt)
-            acc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw), q[qt][s], acc[t][qt],
-                                                                 0, 0, 0);
         }
-      float p[QT][8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float f = a.scale_log2;
-        if constexpr (G::W8) f *= r.ks[e >> 2][e & 3];
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) p[qt][e] = acc[e >> 2][qt][e & 3] * f;
+      if constexpr (G::W8) {
+        if (u + 1 < ulast) load_k(r, u + 1);
       }
-      // all keys take part but in a sequence's last step or on a bad page
-      if (key0 + 32 > en.len || __builtin_amdgcn_ballot_w64(!r.there) != 0) {
-        asm volatile("");                          // a branch that is rarely taken, not selects
-        const int left = en.len - key0 - kv8;
+      int on = 0xff;
+      if (__builtin_expect(!whole, 0)) {           // the sequence's last keys, or a bad page
+        asm volatile("");
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (!r.there || e >= left) {
+          if (!there || kv8 + e >= left) {
+            on &= ~(1 << e);
+            f[e] = 1.0f;
             if constexpr (G::W8) r.vs[e >> 2][e & 3] = 0.0f;
 #pragma unroll
             for (int d = 0; d < G::NW; ++d) r.v[e][d] = 0;
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt) p[qt][e] = -INFINITY;
           }
       }
-      st.weigh(p);
-      if constexpr (G::W8) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < 8; ++e) z[e] = G::W8 ? r.vs[e >> 2][e & 3] : 1.0f;
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt) p[qt][e] *= r.vs[e >> 2][e & 3];
+      for (int qt = 0; qt < QT; ++qt) {
+        if constexpr (QT > 1) __builtin_amdgcn_sched_barrier(0);   // one tile's logits at a time
+        f32x4 s[2];
+        scores(kw, qt, s);
+        if (__builtin_expect(!whole, 0)) {
+          asm volatile("");
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (!(on >> e & 1)) s[e >> 2][e & 3] = -INFINITY;
+        }
+        st.weigh(qt, s, f, z, G::W8);
       }
-      bf16x8 wp[NP][QT];
-      weight_operands<QT, NP>(p, wp);
+      if constexpr (!G::W8) {
+        if (u + 1 < ulast) load_k(r, u + 1);
+      }
       if constexpr (G::W8) {
 #pragma unroll
         for (int d = 0; d < G::NW; ++d) {
@@ -335,30 +374,25 @@ void cache_attn_kernel(CacheAttnArgs a) {
           transpose8(r.v, d, t);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const u32x2 y = widen4<FMT>(t[j][0]), z = widen4<FMT>(t[j][1]);
-            pv_tile<D, QT, NP>(st, 4 * d + j, __builtin_bit_cast(bf16x8, u32x4{y[0], y[1], z[0], z[1]}), wp);
+            const u32x2 y = widen4<FMT>(t[j][0]), c = widen4<FMT>(t[j][1]);
+            st.add(4 * d + j, __builtin_bit_cast(bf16x8, u32x4{y[0], y[1], c[0], c[1]}));
           }
         }
       } else {
 #pragma unroll
         for (int j = 0; j < JT; ++j) {
           if (j % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-          pv_tile<D, QT, NP>(st, j, v_operand16(r.v, j), wp);
+          st.add(j, v_operand16(r.v, j));
         }
       }
+      if (u + 1 < ulast) load_v(r);
     };
     if (u0 < ulast) {
-      Raw<FMT, D> r0, r1;
+      Raw<FMT, D> r;
       load_pages(u0);
-      load(r0, u0);
-      for (int u = u0;; u += 2) {
-        if (u + 1 < ulast) load(r1, u + 1);
-        work_on(r0, u);
-        if (u + 1 >= ulast) break;
-        if (u + 2 < ulast) load(r0, u + 2);
-        work_on(r1, u + 1);
-        if (u + 2 >= ulast) break;
-      }
+      load_k(r, u0);
+      load_v(r);
+      for (int u = u0; u < ulast; ++u) work_on(r, u);
     }
 
     // ---- drafted keys ----
@@ -366,18 +400,19 @@ void cache_attn_kernel(CacheAttnArgs a) {
     const uint16_t* vn = static_cast<const uint16_t*>(a.vn.p) + b * a.vn.sb + h * a.vn.sh;
     // which of its eight keys the lane's column sees
     auto seen_drafts = [&](int qt, int key0) {
-      const int t = max(tok[qt], 0);
-      const uint8_t* mk = a.mask ? a.mask + b * a.mask_b + (int64_t)t * a.T : nullptr;
+      int t, head;
+      row_of(qt, t, head);
+      const uint8_t* mk = a.mask ? a.mask + b * a.mask_b + (int64_t)max(t, 0) * a.T : nullptr;
       int seen = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int key = key0 + kv8 + e;
-        seen |= tok[qt] >= 0 && key < en.cnt && (mk ? mk[min(key, a.T - 1)] != 0 : key <= t) ? 1 << e : 0;
+        seen |= t >= 0 && key < en.cnt && (mk ? mk[min(key, a.T - 1)] != 0 : key <= t) ? 1 << e : 0;
       }
       return seen;
     };
     // a drafted value row's channels of this lane; zero behind the last token
-    auto load_v = [&](int key, uint32_t (&v)[JT / 2]) {
+    auto load_vn = [&](int key, uint32_t (&v)[JT / 2]) {
       const uint16_t* vp = vn + min(key, en.cnt - 1) * a.vn.sn + min(i16, G::VR - 1) * JT;
 #pragma unroll
       for (int d = 0; d < JT / 2; ++d) {
@@ -386,44 +421,42 @@ void cache_attn_kernel(CacheAttnArgs a) {
       }
     };
     bool not_finite = false;
+#pragma unroll 1
     for (int u = max(u0, en.cached_units); u < u1; ++u) {
       const int key0 = (u - en.cached_units) * kUnit + 32 * w;
       if (!drafts || key0 >= en.cnt) break;
-      f32x4 acc[2][QT];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) acc[t][qt] = f32x4{};
+      u32x4 kw[2][KS];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const uint16_t* kp = kn + min(key0 + kq + 4 * t + (i16 & 3), en.cnt - 1) * a.kn.sn;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          bf16x8 kw{};
           const int d = chan<G::W8>(s, g);
-          if (d < D) kw = *reinterpret_cast<const bf16x8*>(kp + d);
-#pragma unroll
-          for (int qt = 0; qt < QT; ++qt)
-            acc[t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kw, q[qt][s], acc[t][qt], 0, 0, 0);
+          kw[t][s] = *reinterpret_cast<const u32x4*>(kp + min(d, D - 8));
+          if (D == 112 && d >= D) kw[t][s] = u32x4{};
         }
       }
       uint32_t v[8][JT / 2];
       bool odd = false;                            // a value that is not finite
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        load_v(key0 + kv8 + e, v[e]);
+        load_vn(key0 + kv8 + e, v[e]);
 #pragma unroll
         for (int d = 0; d < JT / 2; ++d)
           odd |= (v[e][d] & 0x7F800000u) == 0x7F800000u || (v[e][d] & 0x7F80u) == 0x7F80u;
       }
-      float p[QT][8];
+      const float f[8] = {a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2,
+                          a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
+        f32x4 s[2];
+        scores(kw, qt, s);
         const int seen = seen_drafts(qt, key0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[qt][e] = seen >> e & 1 ? acc[e >> 2][qt][e & 3] * a.scale_log2 : -INFINITY;
+        for (int e = 0; e < 8; ++e)
+          if (!(seen >> e & 1)) s[e >> 2][e & 3] = -INFINITY;
+        st.weigh(qt, s, f, f, false);
       }
-      st.weigh(p);
       if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
         not_finite = true;                         // 0 * Inf would reach rows that do not see it: added below
 #pragma unroll
@@ -434,12 +467,9 @@ void cache_attn_kernel(CacheAttnArgs a) {
             if ((v[e][d] & 0x7F80u) == 0x7F80u) v[e][d] &= 0xFFFF0000u;
           }
       }
-      bf16x8 wp[NP][QT];
-      weight_operands<QT, NP>(p, wp);
 #pragma unroll
-      for (int j = 0; j < JT; ++j) pv_tile<D, QT, NP>(st, j, v_operand16(v, j), wp);
+      for (int j = 0; j < JT; ++j) st.add(j, v_operand16(v, j));
     }
-
     // Inf or NaN among the drafted values (never in practice) were left out of the products.
     // For +Inf, -Inf and NaN in turn, a matrix of ones where V holds one is multiplied with
     // the rows' masks, and a sum above zero adds that value to the rows that see it.
@@ -449,17 +479,19 @@ void cache_attn_kernel(CacheAttnArgs a) {
         const int key0 = (u - en.cached_units) * kUnit + 32 * w;
         if (key0 >= en.cnt) break;
         uint32_t v[8][JT / 2];
-        float one[QT][8];
-        bf16x8 mask_op[1][QT];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) load_v(key0 + kv8 + e, v[e]);
+        for (int e = 0; e < 8; ++e) load_vn(key0 + kv8 + e, v[e]);
+        bf16x8 mask_op[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
           const int seen = seen_drafts(qt, key0);
+          float one[1][8];
+          bf16x8 part[1][1];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) one[qt][e] = seen >> e & 1 ? 1.0f : 0.0f;
+          for (int e = 0; e < 8; ++e) one[0][e] = seen >> e & 1 ? 1.0f : 0.0f;
+          weight_operands<1, 1>(one, part);
+          mask_op[qt] = part[0][0];
         }
-        weight_operands<QT, 1>(one, mask_op);
 #pragma unroll 1
         for (int kind = 0; kind < 3; ++kind) {
           const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : NAN);
@@ -480,7 +512,7 @@ void cache_attn_kernel(CacheAttnArgs a) {
             const bf16x8 marks = v_operand16(t, 0);
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
-              const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, mask_op[0][qt], f32x4{}, 0, 0, 0);
+              const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, mask_op[qt], f32x4{}, 0, 0, 0);
 #pragma unroll
               for (int r = 0; r < 4; ++r) st.o[j][qt][r] += y[r] > 0.0f ? add : 0.0f;
             }
@@ -505,6 +537,8 @@ void cache_attn_kernel(CacheAttnArgs a) {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       const int row = qt * 16 + i16;
+      int tok, head;
+      row_of(qt, tok, head);
       float top = sm[0][row];
 #pragma unroll
       for (int k = 1; k < kWaves; ++k) top = fmaxf(top, sm[k][row]);
@@ -533,14 +567,14 @@ void cache_attn_kernel(CacheAttnArgs a) {
           part[PT::ref(QT, row)] = top;
           part[PT::sum(QT, row)] = l;
         }
-      } else if (tok[qt] >= 0) {
+      } else if (tok >= 0) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // NaN stays NaN
         const int d0 = JT * (4 * g + w);
 #pragma unroll
         for (int j = 0; j < JT; ++j) y[j] = l == 0.0f ? 0.0f : y[j] * inv;
-        if (d0 < D) store_row<D>(a, b, head[qt], tok[qt], d0, y);
+        if (d0 < D) store_row<D>(a, b, head, tok, d0, y);
         if (a.lse && w == 0 && g == 0)
-          a.lse[((int64_t)b * a.H + head[qt]) * a.T + tok[qt]] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
+          a.lse[((int64_t)b * a.H + head) * a.T + tok] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
       }
       __syncthreads();
     }

@@ -23,6 +23,11 @@ namespace cattn {
 constexpr int kUnit = 128;       // keys of a unit
 constexpr int kWaves = 4;
 
+// Workgroups per CU (waves per SIMD) of cache_attn_kernel with QT row tiles: at D = 64 and
+// one tile a third finds its registers, and brings 943 MB from 102 us to 90; at D = 128 it
+// would spill (137 us to 155 for 840 MB)
+constexpr int wave_residents(int D, int QT) { return D == 64 && QT == 1 ? 3 : 2; }
+
 struct Entry {                   // one batch entry
   int len;                       // cached tokens
   int cnt;                       // drafted tokens
