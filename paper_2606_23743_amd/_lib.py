@@ -732,42 +732,81 @@ def token_scatter(y_kept, kept_pos, base, out=None, stream=None):
 
 # ------------------------------------- rotary positions, the key/value cache
 
-def _device_of(t, name):
-    """Calls launch on the current device's streams: its tensors have to be there."""
+# (As above, these calls' time is this module's own where tensors are small: a tensor that is
+# as it should be passes one test, and what is wrong with another is found out afterwards.)
+
+def _device() -> int:
+    """The current device, on whose streams calls are launched."""
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getDevice", None)
+    return raw() if raw is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+
+
+def _stream_on(stream, dev: int):
+    return _stream(stream) if stream is not None else _torch()._C._cuda_getCurrentRawStream(dev)
+
+
+def _refuse(t, dtype, shape, name, dev=None):
+    """Raises for a tensor that is not on the current device, or of another type or shape."""
     torch = _torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-
-
-def _heads(t, dtype, shape, name) -> Heads:
-    """A tensor [B, H, N, D] with any strides, its channels contiguous."""
-    _device_of(t, name)
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
+    dev = _device() if dev is None else dev
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+    if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _on_device(t, name):
+    """A tensor on the current device; which device that is."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    dev = _device()
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+    return dev
+
+
+def _heads(t, dtype, shape, name, dev) -> Heads:
+    """A tensor [B, H, N, D] with any strides, its channels contiguous."""
+    if not (isinstance(t, _torch().Tensor) and t.dtype == dtype and t.shape == shape and t.get_device() == dev):
+        _refuse(t, dtype, shape, name, dev)
     sb, sh, sn, sd = t.stride()
     if sd != 1 and shape[3] > 1:
         raise ValueError(f"{name}'s channels must be contiguous (stride 1), got stride {sd}")
     return Heads(t.data_ptr(), shape[1], sb, sh, sn)
 
 
-def _rows_of_ints(t, batch, columns, name):
+def _plain(t, dtype, shape, name, dev) -> int:
+    """A contiguous tensor's pointer."""
+    if not (isinstance(t, _torch().Tensor) and t.dtype == dtype and t.shape == shape and t.get_device() == dev
+            and t.is_contiguous()):
+        _refuse(t, dtype, shape, name, dev)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_of_ints(t, batch, columns, name, dev):
     """int32 [batch, columns] or [columns] (shared): its pointer and batch stride."""
     torch = _torch()
-    _device_of(t, name)
-    if t.dtype != torch.int32:
-        raise TypeError(f"{name} must be {torch.int32}, got {t.dtype}")
-    if t.dim() == 1 and t.shape[0] == columns:
-        step, stride = t.stride(0), 0
-    elif t.dim() == 2 and t.shape[0] == batch and t.shape[1] == columns:
+    if not (isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.get_device() == dev):
+        _refuse(t, torch.int32, getattr(t, "shape", ()), name, dev)
+    shape = t.shape
+    if len(shape) == 2 and shape[0] == batch and shape[1] == columns:
         stride, step = t.stride()
+    elif len(shape) == 1 and shape[0] == columns:
+        step, stride = t.stride(0), 0
     else:
-        raise ValueError(f"{name} must have shape {(batch, columns)} or {(columns,)}, got {tuple(t.shape)}")
+        raise ValueError(f"{name} must have shape {(batch, columns)} or {(columns,)}, got {tuple(shape)}")
     if step != 1 and columns > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
     return t.data_ptr(), stride
@@ -827,31 +866,32 @@ def rotary(plan: dict, positions, q, k=None, q_out=None, k_out=None, backward: b
     torch = _torch()
     if not isinstance(q, torch.Tensor) or q.dim() != 4:
         raise ValueError("q must be a tensor [B, H, N, D]")
-    B, H, N, D = q.shape
+    shp = q.shape
+    B, H, N, D = shp
     if D != plan["head_dim"]:
         raise ValueError(f"q has {D} channels, the plan {plan['head_dim']}")
     dt, code = _dtype_code(q.dtype, "q")
-    qi = _heads(q, dt, q.shape, "q")
+    dev = _on_device(q, "q")
+    qi = _heads(q, dt, shp, "q", dev)
     if q_out is None:
         q_out = torch.empty_like(q)
-    qo = _heads(q_out, dt, q.shape, "q_out")
+    qo = _heads(q_out, dt, shp, "q_out", dev)
     ki = ko = None
     if k is not None:
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("k must be a tensor [B, H, N, D]")
-        shp = torch.Size((B, k.shape[1], N, D))
-        ki = _heads(k, dt, shp, "k")
+        shp = (B, k.shape[1], N, D)
+        ki = _heads(k, dt, shp, "k", dev)
         if k_out is None:
             k_out = torch.empty_like(k)
-        ko = _heads(k_out, dt, shp, "k_out")
+        ko = _heads(k_out, dt, shp, "k_out", dev)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    freq = plan["freq"]
-    _device_of(freq, "plan['freq']")
-    pos, pos_b = _rows_of_ints(positions, B, N, "positions")
-    prm = RotaryParams(B, N, D, plan["rot_dim"], SVA_ROTARY_LAYOUTS[plan["layout"]], code, 1 if backward else 0,
-                       plan["magnitude"])
-    _check(load().sva_rotary(prm, freq.data_ptr(), pos, pos_b, qi, qo, ki, ko, _stream(stream)), "sva_rotary")
+    freq, rot = plan["freq"], plan["rot_dim"]
+    pos, pos_b = _rows_of_ints(positions, B, N, "positions", dev)
+    prm = RotaryParams(B, N, D, rot, SVA_ROTARY_LAYOUTS[plan["layout"]], code, 1 if backward else 0, plan["magnitude"])
+    _check(load().sva_rotary(prm, _plain(freq, torch.float64, (rot // 2,), "plan['freq']", dev), pos, pos_b, qi, qo, ki,
+                             ko, _stream_on(stream, dev)), "sva_rotary")
     _record(stream, q, k, q_out, k_out, freq, positions)
     return q_out, k_out
 
@@ -873,28 +913,25 @@ def kv_cache(num_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, 
     return cache
 
 
-def _cache(c: dict) -> Cache:
+def _cache(c: dict, dev=None) -> Cache:
     torch = _torch()
     k, v = c["k"], c["v"]
-    _device_of(k, "cache['k']")
-    fmt = {torch.bfloat16: 0, torch.uint8: 1, torch.int8: 2}.get(k.dtype)
+    if dev is None:
+        dev = _on_device(k, "cache['k']")
+    dt = k.dtype
+    fmt = 1 if dt == torch.uint8 else 2 if dt == torch.int8 else 0 if dt == torch.bfloat16 else None
     if fmt is None:
-        raise TypeError(f"cache['k'] must be bfloat16, uint8 (e4m3) or int8, got {k.dtype}")
-    if k.dim() != 4:
-        raise ValueError("cache['k'] must be [pages, kv_heads, page_size, head_dim]")
+        raise TypeError(f"cache['k'] must be bfloat16, uint8 (e4m3) or int8, got {dt}")
     shp = k.shape
-    _need(k, k.dtype, shp, "cache['k']")
-    _need(v, k.dtype, shp, "cache['v']")
-    _device_of(v, "cache['v']")
+    if len(shp) != 4:
+        raise ValueError("cache['k'] must be [pages, kv_heads, page_size, head_dim]")
+    kp, vp = _plain(k, dt, shp, "cache['k']", dev), _plain(v, dt, shp, "cache['v']", dev)
     ks = vs = None
     if fmt:
-        ks, vs = c["k_scale"], c["v_scale"]
-        _need(ks, torch.float32, shp[:3], "cache['k_scale']")
-        _need(vs, torch.float32, shp[:3], "cache['v_scale']")
-        _device_of(ks, "cache['k_scale']")
-        _device_of(vs, "cache['v_scale']")
-        ks, vs = ks.data_ptr(), vs.data_ptr()
-    return Cache(fmt, shp[0], shp[1], shp[2], shp[3], k.data_ptr(), v.data_ptr(), ks, vs)
+        rows = shp[:3]
+        ks = _plain(c["k_scale"], torch.float32, rows, "cache['k_scale']", dev)
+        vs = _plain(c["v_scale"], torch.float32, rows, "cache['v_scale']", dev)
+    return Cache(fmt, shp[0], shp[1], shp[2], shp[3], kp, vp, ks, vs)
 
 
 def cache_write(cache: dict, k, v, slots, stream=None) -> dict:
@@ -903,18 +940,20 @@ def cache_write(cache: dict, k, v, slots, stream=None) -> dict:
     place; out of range: nothing is written; the others distinct),
     sva_cache_write.  Returns the cache."""
     torch = _torch()
-    st = _cache(cache)
-    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+    dev = _on_device(k, "k")
+    st = _cache(cache, dev)
+    if k.dim() != 4:
         raise ValueError("k must be a tensor [B, kv_heads, N, D]")
     dt, code = _dtype_code(k.dtype, "k")
     B, _, N, _ = k.shape
-    shp = torch.Size((B, st.kv_heads, N, st.head_dim))
-    hk, hv = _heads(k, dt, shp, "k"), _heads(v, dt, shp, "v")
-    if slots.dim() == 1 and B > 1:
+    shp = (B, st.kv_heads, N, st.head_dim)
+    hk, hv = _heads(k, dt, shp, "k", dev), _heads(v, dt, shp, "v", dev)
+    ptr, sb = _rows_of_ints(slots, B, N, "slots", dev)
+    if B > 1 and slots.dim() == 1:
         raise ValueError("slots must be [B, N]: entries cannot share slots")
-    ptr, sb = _rows_of_ints(slots, B, N, "slots")
-    _check(load().sva_cache_write(st, B, N, code, hk, hv, ptr, sb, _stream(stream)), "sva_cache_write")
-    _record(stream, k, v, slots, *cache.values())
+    _check(load().sva_cache_write(st, B, N, code, hk, hv, ptr, sb, _stream_on(stream, dev)), "sva_cache_write")
+    if stream is not None:
+        _record(stream, k, v, slots, *cache.values())
     return cache
 
 
@@ -923,20 +962,22 @@ def cache_read(cache: dict, slots, k=None, v=None, dtype="bf16", stream=None) ->
     [B, kv_heads, N, D] of dtype ("bf16" or "f32"), sva_cache_read; contiguous
     where allocated here, as the whole-sequence operators take them."""
     torch = _torch()
-    st = _cache(cache)
-    if not isinstance(slots, torch.Tensor) or slots.dim() != 2:
+    dev = _on_device(slots, "slots")
+    st = _cache(cache, dev)
+    if slots.dim() != 2:
         raise ValueError("slots must be a tensor [B, N]")
     B, N = slots.shape
     dt, code = _dtype_code(dtype, "dtype")
-    shp = torch.Size((B, st.kv_heads, N, st.head_dim))
-    ptr, sb = _rows_of_ints(slots, B, N, "slots")
+    shp = (B, st.kv_heads, N, st.head_dim)
+    ptr, sb = _rows_of_ints(slots, B, N, "slots", dev)
     if k is None:
         k = torch.empty(shp, dtype=dt, device=slots.device)
     if v is None:
         v = torch.empty(shp, dtype=dt, device=slots.device)
-    _check(load().sva_cache_read(st, B, N, code, ptr, sb, _heads(k, dt, shp, "k"), _heads(v, dt, shp, "v"),
-                                 _stream(stream)), "sva_cache_read")
-    _record(stream, k, v, slots, *cache.values())
+    _check(load().sva_cache_read(st, B, N, code, ptr, sb, _heads(k, dt, shp, "k", dev), _heads(v, dt, shp, "v", dev),
+                                 _stream_on(stream, dev)), "sva_cache_read")
+    if stream is not None:
+        _record(stream, k, v, slots, *cache.values())
     return k, v
 
 
@@ -963,64 +1004,66 @@ def cache_attention(cache: dict, q, page_table, lengths, k_new=None, v_new=None,
     tensor of cache_attention_workspace bytes (allocated when None).  Returns
     (out, lse)."""
     torch = _torch()
-    st = _cache(cache)
-    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+    dev = _on_device(q, "q")
+    st = _cache(cache, dev)
+    shp = q.shape
+    if len(shp) != 4:
         raise ValueError("q must be a tensor [B, H, T, D]")
-    B, H, T, D = q.shape
+    B, H, T, D = shp
     if D != st.head_dim:
         raise ValueError(f"q has {D} channels, the cache {st.head_dim}")
-    hq = _heads(q, torch.bfloat16, q.shape, "q")
-    _need(lengths, torch.int32, (B,), "lengths")
-    _device_of(lengths, "lengths")
+    bf16, i32 = torch.bfloat16, torch.int32
+    hq = _heads(q, bf16, shp, "q", dev)
+    lens = _plain(lengths, i32, (B,), "lengths", dev)
     if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be a tensor [B, max_pages]")
-    _need(page_table, torch.int32, (B, page_table.shape[1]), "page_table")
-    _device_of(page_table, "page_table")
-    hk = hv = None
+    pages = page_table.shape[1]
+    table = _plain(page_table, i32, (B, pages), "page_table", dev)
+    hk = hv = mk = cnt = None
     if (k_new is None) != (v_new is None):
         raise ValueError("k_new and v_new go together")
     if k_new is not None:
-        shp = torch.Size((B, st.kv_heads, T, D))
-        hk, hv = _heads(k_new, torch.bfloat16, shp, "k_new"), _heads(v_new, torch.bfloat16, shp, "v_new")
+        new = (B, st.kv_heads, T, D)
+        hk, hv = _heads(k_new, bf16, new, "k_new", dev), _heads(v_new, bf16, new, "v_new", dev)
     mask_b = 0
     if mask is not None:
         if k_new is None:
             raise ValueError("mask without drafted keys")
-        _device_of(mask, "mask")
-        if mask.dtype not in (torch.uint8, torch.bool):
+        _on_device(mask, "mask")
+        if mask.dtype != torch.uint8 and mask.dtype != torch.bool:
             raise TypeError(f"mask must be uint8 or bool, got {mask.dtype}")
-        if mask.shape not in ((B, T, T), (T, T)):
+        if mask.shape != (B, T, T) and mask.shape != (T, T):
             raise ValueError(f"mask must have shape {(B, T, T)} or {(T, T)}, got {tuple(mask.shape)}")
-        if mask.stride(-1) != 1 and T > 1 or mask.stride(-2) != T and T > 1:
+        strides = mask.stride()
+        if T > 1 and (strides[-1] != 1 or strides[-2] != T):
             raise ValueError("mask's last two dimensions must be contiguous")
-        mask_b = mask.stride(0) if mask.dim() == 3 else 0
+        mask_b = strides[0] if len(strides) == 3 else 0
+        mk = mask.data_ptr()
     if counts is not None:
-        _need(counts, torch.int32, (B,), "counts")
-        _device_of(counts, "counts")
+        cnt = _plain(counts, i32, (B,), "counts", dev)
     if out is None:
         dt, code = _dtype_code(out_dtype, "out_dtype")
         out = torch.empty_like(q, dtype=dt)
     else:
         dt, code = _dtype_code(out.dtype, "out")
-    ho = _heads(out, dt, q.shape, "out")
+    ho = _heads(out, dt, shp, "out", dev)
     if want_lse and lse is None:
         lse = torch.empty((B, H, T), dtype=torch.float32, device=q.device)
-    if lse is not None:
-        _need(lse, torch.float32, (B, H, T), "lse")
-        _device_of(lse, "lse")
-    qry = CacheQuery(B, H, T, page_table.shape[1], float(softmax_scale), code)
+    lp = None if lse is None else _plain(lse, torch.float32, (B, H, T), "lse", dev)
+    qry = CacheQuery(B, H, T, pages, float(softmax_scale), code)
     lib = load()
+    ws_ptr, ws_bytes = None, 0
     if workspace is None:
         need = ctypes.c_size_t(0)
-        _check(lib.sva_cache_attention_workspace(st, qry, ctypes.byref(need)), "sva_cache_attention_workspace")
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
-    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 device tensor")
+        _check(lib.sva_cache_attention_workspace(st, qry, need), "sva_cache_attention_workspace")
+        if need.value:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+            ws_ptr, ws_bytes = workspace.data_ptr(), need.value
     else:
-        _device_of(workspace, "workspace")
-    ws_ptr, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    _check(lib.sva_cache_attention(st, qry, hq, page_table.data_ptr(), lengths.data_ptr(), hk, hv, _ptr(mask), mask_b,
-                                   _ptr(counts), ws_ptr, ws_bytes, ho, _ptr(lse), _stream(stream)),
-           "sva_cache_attention")
-    _record(stream, q, page_table, lengths, k_new, v_new, mask, counts, workspace, out, lse, *cache.values())
+        ws_bytes = workspace.numel()
+        ws_ptr = _plain(workspace, torch.uint8, (ws_bytes,), "workspace", dev)
+    _check(lib.sva_cache_attention(st, qry, hq, table, lens, hk, hv, mk, mask_b, cnt, ws_ptr, ws_bytes, ho, lp,
+                                   _stream_on(stream, dev)), "sva_cache_attention")
+    if stream is not None:
+        _record(stream, q, page_table, lengths, k_new, v_new, mask, counts, workspace, out, lse, *cache.values())
     return out, lse

@@ -221,7 +221,12 @@ void cache_attn_kernel(CacheAttnArgs a) {
     bf16x8 q1[KS];                                 // one tile stays in registers, more lie in LDS
     if constexpr (QT == 1) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) q1[s] = __builtin_bit_cast(bf16x8, load_q(0, s));
+      for (int s = 0; s < KS; ++s) {
+        q1[s] = __builtin_bit_cast(bf16x8, load_q(0, s));
+        // it has landed here: without this use the compiler waits for it again in every step,
+        // and with it for the codes that are on their way
+        asm volatile("" : "+v"(q1[s]));
+      }
     } else {
 #pragma unroll 1
       for (int qt = w; qt < QT; qt += kWaves)

@@ -99,6 +99,12 @@ void cache_tile_kernel(CacheAttnArgs a) {
         else q[qt][s] = bf16x8{};
       }
     }
+    // Q has landed here: without this use the compiler waits for it again in every step, and
+    // with it for the codes that are on their way
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+      for (int s = 0; s < G16::KS; ++s) asm volatile("" : "+v"(q[qt][s]));
     // a wave without rows stages its share and computes nothing
     const bool busy = rt * RPT + w * QT * 16 < en.cnt * a.G;
 
@@ -124,6 +130,7 @@ void cache_tile_kernel(CacheAttnArgs a) {
       bool keep[NR];                               // whether the piece is a key's
       bool lost;                                   // a key's page does not exist
       float scale;
+      bool scaled;                                 // whether the scale is a key's
     };
     const float* scales = threadIdx.x < kChunk ? a.c.ks : a.c.vs;
     auto load_pages = [&](int c) {
@@ -132,7 +139,9 @@ void cache_tile_kernel(CacheAttnArgs a) {
       for (int r = 0; r < NR; ++r) pg[r] = page_at(key0 + srow + r * RPP);
       if constexpr (W8) spg = page_at(key0 + (threadIdx.x & (kChunk - 1)));
     };
-    // chunk c's codes, with the pages loaded for it; then the next chunk's pages
+    // chunk c's codes, with the pages loaded for it, and the next chunk's pages.  Lanes without
+    // a key, and all of them past the last chunk, load the cache's first bytes: loads under a
+    // condition make the compiler wait for all of them where it needs the older ones only.
     auto load_codes = [&](Raw& x, int c) {
       const int key0 = k0 + c * kChunk;
       int64_t at[NR], sat = 0;
@@ -142,24 +151,24 @@ void cache_tile_kernel(CacheAttnArgs a) {
       for (int r = 0; r < NR; ++r) {
         const int key = key0 + srow + r * RPP;
         const bool in = key < k1 && pg[r] >= 0 && pg[r] < a.c.num_pages;
-        at[r] = ((((in ? (int64_t)pg[r] : 0) * Hkv + h) << log2p) + (key & pmask)) * (D * EB) + min(piece, PIECES - 1) * 16;
+        at[r] = in ? ((((int64_t)pg[r] * Hkv + h) << log2p) + (key & pmask)) * (D * EB) + min(piece, PIECES - 1) * 16 : 0;
         x.keep[r] = in && piece < PIECES;
         x.lost |= key < k1 && !in;
       }
       if constexpr (W8) {
         const int key = key0 + (threadIdx.x & (kChunk - 1));
         sin = key < k1 && spg >= 0 && spg < a.c.num_pages;
-        sat = (((sin ? (int64_t)spg : 0) * Hkv + h) << log2p) + (key & pmask);
+        sat = sin ? (((int64_t)spg * Hkv + h) << log2p) + (key & pmask) : 0;
       }
-      if (c + 1 < nc) load_pages(c + 1);
+      load_pages(c + 1);                           // (past the end: the table's last column)
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         x.k[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.c.k) + at[r]));
         x.v[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.c.v) + at[r]));
       }
       if constexpr (W8) {
-        const float y = threadIdx.x < 2 * kChunk ? scales[sat] : 0.0f;
-        x.scale = sin ? y : 0.0f;
+        x.scale = scales[sat];                     // (the upper half of the lanes loads V's again)
+        x.scaled = sin;
       }
     };
     auto write_stage = [&](const Raw& x, int st) {
@@ -184,8 +193,9 @@ void cache_tile_kernel(CacheAttnArgs a) {
         }
       }
       if constexpr (W8) {
-        if (threadIdx.x < kChunk) fs[st][threadIdx.x] = x.scale * a.scale_log2;
-        else if (threadIdx.x < 2 * kChunk) vs[st][threadIdx.x - kChunk] = x.scale;
+        const float y = x.scaled ? x.scale : 0.0f;
+        if (threadIdx.x < kChunk) fs[st][threadIdx.x] = y * a.scale_log2;
+        else if (threadIdx.x < 2 * kChunk) vs[st][threadIdx.x - kChunk] = y;
       }
       const bool any = __builtin_amdgcn_ballot_w64(x.lost) != 0;
       if (lane == 0) lost[st][threadIdx.x >> 6] = any;
@@ -257,7 +267,28 @@ void cache_tile_kernel(CacheAttnArgs a) {
       f32x4 s[NS][2][QT];
       const unsigned char* vt = &Vs[st][sub0 * 32 * G::RB];
 #pragma unroll
-      for (int y = 0; y < NS; ++y) attn::qk16<D>(s[y], &Ks[st][(sub0 + y) * 32 * G::RB], koff, q);
+      for (int y = 0; y < NS; ++y) {
+        // all K operands are read before the first is used: read where they are used, each
+        // was waited for
+        const unsigned char* kt = &Ks[st][(sub0 + y) * 32 * G::RB];
+        bf16x8 kop[G16::KS][2];
+#pragma unroll
+        for (int k = 0; k < G16::KS; ++k)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) kop[k][t] = *reinterpret_cast<const bf16x8*>(kt + koff[k] + t * 16 * G::RB);
+        if constexpr (QT > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) s[y][t][qt] = f32x4{};
+#pragma unroll
+        for (int k = 0; k < G16::KS; ++k)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt)
+              s[y][t][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[k][t], q[qt][k], s[y][t][qt], 0, 0, 0);
+      }
       // V operands are read ahead of the softmax, as many as registers allow: read where
       // they are used, each pair was waited for
       bf16x8 vop[PRE];
@@ -377,11 +408,9 @@ void cache_tile_kernel(CacheAttnArgs a) {
     if (nc > 0) {
       load_pages(0);
       load_codes(raw[0], 0);
-      if constexpr (AHEAD == 2) {
-        if (nc > 1) load_codes(raw[1], 1);
-      }
+      if constexpr (AHEAD == 2) load_codes(raw[1], 1);
       write_stage(raw[0], 0);
-      if (nc > AHEAD) load_codes(raw[0], AHEAD);
+      load_codes(raw[0], AHEAD);
     } else if (nd > 0) {
       __syncthreads();                             // not_finite is clear
       stage_drafts(d0, 0);
@@ -391,7 +420,7 @@ void cache_tile_kernel(CacheAttnArgs a) {
       const int st = c & 1;
       if (c + 1 < nc) {
         write_stage(next, st ^ 1);
-        if (c + 1 + AHEAD < nc) load_codes(next, c + 1 + AHEAD);
+        load_codes(next, c + 1 + AHEAD);
       } else if (c + 1 < nc + nd) {
         stage_drafts(d0 + (c + 1 - nc) * kChunk, st ^ 1);
       }
