@@ -24,6 +24,22 @@ typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
+// Calls past the caches (64 MB) are streamed where that pays; us, plain / non-temporal: 8-bit
+// codes of bf16 rows 138 / 129 (111,600 tokens of 8 heads of 128), 60 / 56 (50,000 of 16 of 64);
+// of float32 rows, and bf16 rows as they are, 188 / 192 and 149 / 152.  Reading back
+// as float32, stores only: 82 / 69 (15,602 of 20 of 112), 200 / 192 (50,000 of 16); as bf16
+// 132 / 136 and 118 / 114.
+template <bool NT, class T>
+__device__ __forceinline__ T load(const T* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  return *p;
+}
+template <bool NT, class T>
+__device__ __forceinline__ void store(T* p, T v) {
+  if constexpr (NT) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -61,22 +77,40 @@ __device__ __forceinline__ int e4m3_exp(float amax) {
   return e < -127 ? -127 : (e > 127 ? 127 : e);
 }
 
-// x / s to the nearest whole number, ties to even, in [-127, 127]: the rounded
-// product may be one off next to a half step, which the exact residual x - k s
-// shows (its difference from s/2 is a multiple of ulp(s)/2: one fma holds it)
-__device__ __forceinline__ float int8_code(float x, float s, float inv, float half) {
-  float k = rintf(x * inv);
-  const float r = fmaf(-k, s, x);
-  const float far = fabsf(r);
-  const bool odd = ((int)k & 1) != 0;
-  if (far > half || (far == half && odd)) k += copysignf(1.0f, r);
-  return fminf(fmaxf(k, -127.0f), 127.0f);
-}
-
-__device__ __forceinline__ uint32_t bytes4(float a, float b, float c, float d) {
-  const uint32_t lo = ((uint32_t)(int)a & 255u) | (((uint32_t)(int)b & 255u) << 8);
-  const uint32_t hi = ((uint32_t)(int)c & 255u) | (((uint32_t)(int)d & 255u) << 8);
-  return lo | (hi << 16);
+// Eight x / s to the nearest whole numbers, ties to even, as bytes.  x times the rounded
+// reciprocal, plus 1.5 * 2^23, has the whole number in its low bits; it may be one off next to
+// a half step, which the exact residual x - k s shows (its difference from s/2 is a multiple
+// of ulp(s)/2: one fma holds it).  Residuals below half a step prove all eight right; else,
+// rarely, each is looked at.  (Looked at every time, the instructions bound the kernel: 108 us
+// for 2 x 16,380 tokens of 20 heads of 112.)
+__device__ __forceinline__ u32x2 int8_codes(const float (&x)[8], float s, bool lifted) {
+  constexpr float kWhole = 12582912.0f;
+  const float inv = 1.0f / s, half = 0.5f * s;
+  float t[8], far = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    t[e] = fmaf(x[e], inv, kWhole);
+    far = fmaxf(far, fabsf(fmaf(-(t[e] - kWhole), s, x[e])));
+  }
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(far >= half || lifted) != 0, 0)) {
+    asm volatile("");                          // a branch that is rarely taken, not selects
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float k = rintf(x[e] * inv);
+      const float r = fmaf(-k, s, x[e]);
+      const bool odd = ((int)k & 1) != 0;
+      if (fabsf(r) > half || (fabsf(r) == half && odd)) k += copysignf(1.0f, r);
+      t[e] = fminf(fmaxf(k, -127.0f), 127.0f) + kWhole;
+    }
+  }
+  u32x2 o;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(t[4 * w + 1]), __float_as_uint(t[4 * w]), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(t[4 * w + 3]), __float_as_uint(t[4 * w + 2]), 0x04000c0cu);
+    o[w] = lo | hi;
+  }
+  return o;
 }
 
 // eight values -> codes and the row's scale (every lane of the row has it)
@@ -102,13 +136,16 @@ __device__ __forceinline__ u32x2 quantise8(const float (&y)[8], float& scale) {
     scale = m / 127.0f;
     if (!(scale > 0.0f)) scale = 1.0f;
     // tiny rows are lifted by a power of two, so that the reciprocal is finite
-    const float lift = scale < 0x1p-100f ? 0x1p100f : 1.0f;
-    const float s = scale * lift, inv = 1.0f / s, half = 0.5f * s;
-    float k[8];
+    const bool lifted = scale < 0x1p-100f;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(lifted) != 0, 0)) {
+      const float lift = lifted ? 0x1p100f : 1.0f;
+      float z[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) k[e] = int8_code(y[e] * lift, s, inv, half);
-    o[0] = bytes4(k[0], k[1], k[2], k[3]);
-    o[1] = bytes4(k[4], k[5], k[6], k[7]);
+      for (int e = 0; e < 8; ++e) z[e] = y[e] * lift;
+      o = int8_codes(z, scale * lift, true);
+    } else {
+      o = int8_codes(y, scale, false);
+    }
   }
   return o;
 }
@@ -166,7 +203,7 @@ struct Place {
   }
 };
 
-template <int D, int FMT, bool F32>
+template <int D, int FMT, bool F32, bool NT>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs a) {
   using P = Place<D>;
   const P p(a);
@@ -179,10 +216,10 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs a) 
     const int h = min(p.h0 + u, a.c.heads - 1);
     const int64_t at = from + h * x.sh;
     if constexpr (F32) {
-      w[u][0] = *reinterpret_cast<const u32x4*>(static_cast<const float*>(x.p) + at);
-      w[u][1] = *reinterpret_cast<const u32x4*>(static_cast<const float*>(x.p) + at + 4);
+      w[u][0] = load<NT>(reinterpret_cast<const u32x4*>(static_cast<const float*>(x.p) + at));
+      w[u][1] = load<NT>(reinterpret_cast<const u32x4*>(static_cast<const float*>(x.p) + at + 4));
     } else {
-      w[u][0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x.p) + at);
+      w[u][0] = load<NT>(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x.p) + at));
     }
   }
   const bool put = p.here && p.row >= 0;
@@ -211,14 +248,14 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheRowsArgs a) 
       float scale;
       const u32x2 o = quantise8<FMT, P::TPR>(y, scale);
       if (put && p.live) {
-        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(codes) + row * D + p.chunk * 8) = o;
+        store<NT>(reinterpret_cast<u32x2*>(static_cast<uint8_t*>(codes) + row * D + p.chunk * 8), o);
         if (p.chunk == 0) (isv ? a.c.vs : a.c.ks)[row] = scale;
       }
     }
   }
 }
 
-template <int D, int FMT, bool F32>
+template <int D, int FMT, bool F32, bool NT>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs a) {
   const Place<D> p(a);
   const bool isv = blockIdx.y != 0;
@@ -227,21 +264,29 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs a) {
   const float* scales = isv ? a.c.vs : a.c.ks;
   const bool got = p.row >= 0;
   const int64_t row0 = got ? p.row : 0;        // a bad slot reads page 0's first heads, and gives zeros
+  // A lane's eight channels: one piece; for float32 results two runs of four, so that
+  // each of its two stores is contiguous over the lanes
+  constexpr int R = F32 ? 2 : 1, EB = FMT == kCacheBf16 ? 2 : 1;
   using W = std::conditional_t<FMT == kCacheBf16, u32x4, u32x2>;
   W w[kHeads];
+  const int at0 = F32 ? 4 * p.chunk : 8 * p.chunk, at1 = F32 ? at0 + D / 2 : at0 + 4;
   float s[kHeads];
   const int64_t last = got ? (int64_t)(a.c.heads - 1 - p.h0) * p.head_step : 0;
 #pragma unroll
   for (int u = 0; u < kHeads; ++u) {
     const int64_t row = row0 + min((int64_t)u * p.head_step, last);
-    if constexpr (FMT == kCacheBf16) {
-      w[u] = *reinterpret_cast<const W*>(static_cast<const uint16_t*>(codes) + row * D + p.chunk * 8);
+    const uint8_t* from = static_cast<const uint8_t*>(codes) + row * (D * EB);
+    using H = std::conditional_t<FMT == kCacheBf16, u32x2, uint32_t>;
+    if constexpr (R == 1) {
+      w[u] = *reinterpret_cast<const W*>(from + at0 * EB);
     } else {
-      w[u] = *reinterpret_cast<const W*>(static_cast<const uint8_t*>(codes) + row * D + p.chunk * 8);
-      s[u] = scales[row];
+      const H lo = *reinterpret_cast<const H*>(from + at0 * EB), hi = *reinterpret_cast<const H*>(from + at1 * EB);
+      if constexpr (FMT == kCacheBf16) w[u] = W{lo[0], lo[1], hi[0], hi[1]};
+      else w[u] = W{lo, hi};
     }
+    if constexpr (FMT != kCacheBf16) s[u] = scales[row];
   }
-  const int64_t to = p.b * x.sb + p.n * x.sn + p.chunk * 8;
+  const int64_t to = p.b * x.sb + p.n * x.sn;
 #pragma unroll
   for (int u = 0; u < kHeads; ++u) {
     if (p.h0 + u >= a.c.heads) break;          // uniform
@@ -271,11 +316,10 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs a) {
       }
     }
     if constexpr (F32) {
-      u32x4* out = reinterpret_cast<u32x4*>(static_cast<float*>(x.p) + at);
-      out[0] = o[0];
-      out[1] = o[1];
+      store<NT>(reinterpret_cast<u32x4*>(static_cast<float*>(x.p) + at + at0), o[0]);
+      store<NT>(reinterpret_cast<u32x4*>(static_cast<float*>(x.p) + at + at1), o[1]);
     } else {
-      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(x.p) + at) = o[0];
+      store<NT>(reinterpret_cast<u32x4*>(static_cast<uint16_t*>(x.p) + at + at0), o[0]);
     }
   }
 }
@@ -284,8 +328,15 @@ template <int D, int FMT, bool F32>
 void launch_one(const CacheRowsArgs& a, bool write, hipStream_t stream) {
   const int64_t tiles = ((int64_t)a.B * a.N + Place<D>::RPP - 1) / Place<D>::RPP;
   const dim3 grid((unsigned)(tiles * ((a.c.heads + kHeads - 1) / kHeads)), 2);
-  if (write) hipLaunchKernelGGL((cache_write_kernel<D, FMT, F32>), grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((cache_read_kernel<D, FMT, F32>), grid, dim3(kThreads), 0, stream, a);
+  constexpr bool kWriteNT = FMT != kCacheBf16 && !F32, kReadNT = F32;
+  const bool big = (int64_t)a.B * a.N * a.c.heads * D * (F32 ? 4 : 2) >= (64 << 20);
+  if (write) {
+    if (big) hipLaunchKernelGGL((cache_write_kernel<D, FMT, F32, kWriteNT>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((cache_write_kernel<D, FMT, F32, false>), grid, dim3(kThreads), 0, stream, a);
+  } else {
+    if (big) hipLaunchKernelGGL((cache_read_kernel<D, FMT, F32, kReadNT>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((cache_read_kernel<D, FMT, F32, false>), grid, dim3(kThreads), 0, stream, a);
+  }
 }
 
 template <int D>
