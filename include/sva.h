@@ -545,8 +545,8 @@ typedef struct sva_cache_query {
 } sva_cache_query;
 
 /* Bytes of device workspace that sva_cache_attention needs (partial results of
- * keys divided among workgroups, at most 66 MB; the cache's pointers are not
- * read).  Host only. */
+ * keys divided among workgroups, at most 66 MB; none for short page tables;
+ * the cache's pointers are not read).  Host only. */
 int sva_cache_attention_workspace(const sva_cache* cache, const sva_cache_query* query, size_t* bytes);
 
 /* Attention of drafted tokens over a cache and over each other: query token t
@@ -574,8 +574,9 @@ int sva_cache_attention_workspace(const sva_cache* cache, const sva_cache_query*
  *   lse        : float32 [B, H, T] contiguous or NULL; natural-log log-sum-exp of
  *                the scaled logits (-inf for a query that attends to nothing)
  *   workspace  : device memory, 256-byte aligned, at least
- *                sva_cache_attention_workspace bytes; contents on entry do not
- *                matter.  Calls that share one must not overlap.
+ *                sva_cache_attention_workspace bytes (may be NULL where that is
+ *                0); contents on entry do not matter.  Calls that share one must
+ *                not overlap.
  * q, k_new, v_new and out: 16-byte aligned data and strides.  Masked keys and
  * values take no part, whatever they hold.  Codes are widened to bf16 exactly
  * and multiplied by bf16 MFMA with float32 accumulation, the scales applied to

@@ -990,6 +990,9 @@ def cache_attention_workspace(cache: dict, batch: int, heads: int, queries: int,
     return out.value
 
 
+_workspace_bytes = {}      # sva_cache_attention_workspace by sizes
+
+
 def cache_attention(cache: dict, q, page_table, lengths, k_new=None, v_new=None, mask=None, counts=None,
                     softmax_scale: float = 0.0, out_dtype="bf16", out=None, want_lse: bool = False, lse=None,
                     workspace=None, stream=None) -> Tuple:
@@ -1054,11 +1057,17 @@ def cache_attention(cache: dict, q, page_table, lengths, k_new=None, v_new=None,
     lib = load()
     ws_ptr, ws_bytes = None, 0
     if workspace is None:
-        need = ctypes.c_size_t(0)
-        _check(lib.sva_cache_attention_workspace(st, qry, need), "sva_cache_attention_workspace")
-        if need.value:
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-            ws_ptr, ws_bytes = workspace.data_ptr(), need.value
+        sizes = (B, H, T, pages, st.kv_heads, st.page_size, D)
+        ws_bytes = _workspace_bytes.get(sizes)
+        if ws_bytes is None:
+            need = ctypes.c_size_t(0)
+            _check(lib.sva_cache_attention_workspace(st, qry, need), "sva_cache_attention_workspace")
+            if len(_workspace_bytes) > 4096:
+                _workspace_bytes.clear()
+            ws_bytes = _workspace_bytes[sizes] = need.value
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            ws_ptr = workspace.data_ptr()
     else:
         ws_bytes = workspace.numel()
         ws_ptr = _plain(workspace, torch.uint8, (ws_bytes,), "workspace", dev)

@@ -61,6 +61,7 @@ struct CacheAttnArgs {
   int B, H, G, T, max_pages;     // G = H / kv heads
   float scale_log2;
   bool out_f32;
+  bool divide;                   // whether a sequence's keys may be divided among workgroups
 };
 // How a call is run, and its workspace.
 struct CacheAttnShape {

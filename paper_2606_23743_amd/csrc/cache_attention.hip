@@ -141,17 +141,19 @@ CacheAttnShape cache_attn_shape(const CacheAttnArgs& a) {
   // as many workgroups as are resident at once
   const int resident = kCus * (s.shared ? 2 : wave_residents(a.c.D, s.tiles));
   const int cap = a.max_pages << a.c.log2_page;
-  const Entry e = entry_of(cap, a.T, cap, a.T, a.G, 16 * s.tiles, true);
-  const int64_t most = entry_work(e, a.c.heads) * a.B;
+  const Entry e = entry_of(cap, a.T, cap, a.T, a.G, 16 * s.tiles, true, true);
+  s.split = e.units > kWholeUnits;
+  const int64_t most = (int64_t)(s.split ? e.units : 1) * e.tiles * a.c.heads * a.B;
   s.wgs = (int)(most < resident ? most : resident);
-  s.split = e.units > 1;
   const size_t floats = a.c.D > 64 ? Part<128>::floats(s.tiles) : Part<64>::floats(s.tiles);
   s.ws_bytes = s.split ? (size_t)2 * s.wgs * floats * 4 : 0;
   return s;
 }
 
-hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t stream) {
-  const CacheAttnShape s = cache_attn_shape(a);
+hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t stream) {
+  const CacheAttnShape s = cache_attn_shape(args);
+  CacheAttnArgs a = args;
+  a.divide = s.split;
   hipError_t e;
   if (a.c.format == kCacheBf16) e = launch_cache_attention_bf16(a, s, stream);
   else if (a.c.format == kCacheE4m3) e = launch_cache_attention_e4m3(a, s, stream);

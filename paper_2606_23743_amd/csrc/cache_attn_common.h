@@ -71,7 +71,7 @@ struct Finder {
   int64_t total;
 
   __device__ __forceinline__ Entry of(int len, int cnt) const {
-    return entry_of(len, cnt, a.max_pages << a.c.log2_page, a.T, a.G, rows, a.kn.p != nullptr);
+    return entry_of(len, cnt, a.max_pages << a.c.log2_page, a.T, a.G, rows, a.kn.p != nullptr, a.divide);
   }
   // b alike in all lanes
   __device__ __forceinline__ Entry at(int b) const {

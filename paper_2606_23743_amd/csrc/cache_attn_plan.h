@@ -9,7 +9,8 @@
 // length: workgroup i takes units i*U/n .. (i+1)*U/n - 1 of U.  However ragged the
 // lengths, every workgroup then reads the same number of keys; a run may cross
 // segments, and a segment whose units went to several workgroups is joined from
-// their partial results afterwards.  A workgroup leaves at most two of these:
+// their partial results afterwards.  Short caches are not divided (their segments count as
+// one unit each): joining would cost more than it gives.  A workgroup leaves at most two parts:
 // slot 2i for a run that begins inside a segment, 2i + 1 for one that begins with a
 // segment and ends inside it.
 #pragma once
@@ -21,6 +22,11 @@ namespace sva {
 namespace cattn {
 
 constexpr int kUnit = 128;       // keys of a unit
+// Segments of at most so many units are not divided: the join's launch takes longer than the
+// units one after the other (us a call, divided / whole, 8 cache heads of 500 tokens: one
+// sequence 18.4 / 15.8, 64 of them 27.4 / 20.9; 16 of 900 tokens 19.9 / 21.4, one of 1,900
+// 17.6 / 30.6)
+constexpr int kWholeUnits = 6;
 constexpr int kWaves = 4;
 
 // Workgroups per CU (waves per SIMD) of cache_attn_kernel with QT row tiles: at D = 64 and
@@ -33,9 +39,11 @@ struct Entry {                   // one batch entry
   int cnt;                       // drafted tokens
   int cached_units, units;       // of each of its segments
   int tiles;                     // row tiles
+  int span;                      // units of a segment in the division: 1 where segments are not divided
 };
 
-__host__ __device__ __forceinline__ Entry entry_of(int len, int cnt, int max_len, int T, int G, int rows, bool drafts) {
+__host__ __device__ __forceinline__ Entry entry_of(int len, int cnt, int max_len, int T, int G, int rows, bool drafts,
+                                                         bool divide) {
   Entry e;
   e.len = len < 0 ? 0 : (len > max_len ? max_len : len);
   e.cnt = cnt < 0 ? 0 : (cnt > T ? T : cnt);
@@ -43,12 +51,13 @@ __host__ __device__ __forceinline__ Entry entry_of(int len, int cnt, int max_len
   e.units = e.cached_units + (drafts ? (e.cnt + kUnit - 1) / kUnit : 0);
   if (e.units < 1) e.units = 1;
   e.tiles = (int)(((int64_t)e.cnt * G + rows - 1) / rows);
+  e.span = divide ? e.units : 1;
   return e;
 }
 
 // units of all of an entry's segments
 __host__ __device__ __forceinline__ int64_t entry_work(const Entry& e, int kv_heads) {
-  return (int64_t)e.units * e.tiles * kv_heads;
+  return (int64_t)e.span * e.tiles * kv_heads;
 }
 
 // floor(a / b) for 0 <= a < 2^52, b > 0, by a float64 quotient that is at most one off (a

@@ -76,11 +76,11 @@ void cache_tile_kernel(CacheAttnArgs a) {
       ++b;
       continue;
     }
-    const int seg = uniform((int)div_floor(x - ebase, en.units));
-    const int u0 = (int)(x - ebase - (int64_t)seg * en.units);
-    const int u1 = (int)min((int64_t)en.units, u0 + (end - x));
+    const int seg = uniform((int)div_floor(x - ebase, en.span));
+    const int u0 = (int)(x - ebase - (int64_t)seg * en.span);
+    const int u1 = a.divide ? (int)min((int64_t)en.units, u0 + (end - x)) : en.units;
     const int h = uniform(seg / en.tiles), rt = seg - h * en.tiles;
-    x += u1 - u0;
+    x += a.divide ? u1 - u0 : 1;
 
     // ---- Q ----
     bf16x8 q[QT][G16::KS];

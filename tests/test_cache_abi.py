@@ -133,7 +133,7 @@ def test_cache_attention_refusals(lib):
     B, H, T, D = 2, 4, 3, 64
     q, o = heads(A + 4 * MB, H, T, D), heads(A + 5 * MB, H, T, D)
     k, v = heads(A + 6 * MB, 2, T, D), heads(A + 7 * MB, 2, T, D)
-    good = dict(batch=B, heads=H, queries=T, max_pages=2, softmax_scale=0.0, out_dtype=0)
+    good = dict(batch=B, heads=H, queries=T, max_pages=32, softmax_scale=0.0, out_dtype=0)
     need = ctypes.c_size_t()
     assert lib.sva_cache_attention_workspace(a_cache(), CacheQuery(**good), need) == OK and need.value > 0
     W = need.value
@@ -163,8 +163,8 @@ def test_cache_attention_refusals(lib):
                 qry = CacheQuery(**{**good, "queries": t, "heads": h, "max_pages": 4096, "batch": 64})
                 assert lib.sva_cache_attention_workspace(a_cache(d=d), qry, need) == OK
                 assert 0 < need.value <= 66 * 2 ** 20
-    one = CacheQuery(**{**good, "max_pages": 1, "queries": 1})
-    assert lib.sva_cache_attention_workspace(a_cache(), one, need) == OK
+    one = CacheQuery(**{**good, "max_pages": 1, "queries": 1})       # a short cache is not divided
+    assert lib.sva_cache_attention_workspace(a_cache(), one, need) == OK and need.value == 0
     assert lib.sva_cache_attention_workspace(a_cache(), one, None) == BAD
 
 

@@ -32,12 +32,14 @@ int main() {
     for (auto& x : e) {
       const int len = rng() % 4 == 0 ? (int)(rng() % 3) - 1 : (int)(rng() % (max_len + 50));
       const int cnt = rng() % 4 == 0 ? (int)(rng() % (T + 3)) - 1 : T;
-      x = entry_of(len, cnt, max_len, T, G, rows, drafts);
+      x = entry_of(len, cnt, max_len, T, G, rows, drafts, true);
       bad += x.len < 0 || x.len > max_len || x.cnt < 0 || x.cnt > T || x.units < 1;
       bad += (int64_t)x.cached_units * kUnit < x.len || (int64_t)x.tiles * rows < (int64_t)x.cnt * G;
       if (drafts) bad += (int64_t)(x.units - x.cached_units) * kUnit < x.cnt;
       U += entry_work(x, kv);
     }
+    const Entry whole = entry_of(max_len, T, max_len, T, G, rows, drafts, false);
+    bad += entry_work(whole, kv) != (int64_t)whole.tiles * kv;     // undivided: a place for each segment
     if (U == 0) continue;
     const int n = (int)(grid < U ? grid : U);
     int64_t at = 0, least = U, most = 0;

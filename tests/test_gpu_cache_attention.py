@@ -294,8 +294,12 @@ def test_binding_refusals():
         sva.cache_attention(dev, q, t, n, k, v, counts=n[:1])
     with pytest.raises(sva.SvaError):
         sva.cache_attention(dev, q, t, n, k, v, out=q)
+    long_table = torch.zeros((2, 100), dtype=torch.int32, device="cuda")     # past what is left undivided
+    assert sva.cache_attention_workspace(dev, 2, 2, 3, 100) > 256
     with pytest.raises(sva.SvaError):
-        sva.cache_attention(dev, q, t, n, k, v, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+        sva.cache_attention(dev, q, long_table, n, k, v, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(TypeError):
+        sva.cache_attention(dev, q, long_table, n, k, v, workspace=torch.empty(1 << 26, device="cuda"))
 
 
 @pytest.mark.parametrize("fmt,tol", [("bf16", 0.0), ("int8", 0.02), ("e4m3", 0.12)])
