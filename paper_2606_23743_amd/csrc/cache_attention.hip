@@ -28,19 +28,20 @@ __global__ __launch_bounds__(64 * kJoinGroups) void cache_join_kernel(CacheAttnA
   id /= max_tiles;
   const int h = id % a.c.heads, b = id / a.c.heads;
 
-  const Finder fd(a, RPT);
+  const Finder fd(a, RPT, grid_n);
   const Entry en = fd.at(b);
   if (rt >= en.tiles || (rt * RPT + qt * 16) >= en.cnt * a.G) return;
-  const int64_t U = fd.total;
-  const int n = (int)min((int64_t)grid_n, U);
-  // the entry's first unit: the scan up to b
+  const int64_t W = fd.total;
+  const int n = (int)min((int64_t)grid_n, W);
+  // the entry's first place: the scan up to b
   int64_t base = 0;
   for (int b0 = 0; b0 < b; b0 += 64) {
     const int64_t in = a.B <= 64 ? fd.incl : fd.scan(b0);
     base += uniform(__shfl(in, min(b - b0, 64) - 1));
   }
-  const int64_t s0 = base + ((int64_t)h * en.tiles + rt) * en.units;
-  const int i0 = uniform(owner(s0, n, U)), i1 = uniform(owner(s0 + en.units - 1, n, U));
+  const int64_t seg = (int64_t)h * en.tiles + rt;
+  const int i0 = uniform(owner(base + place_of(en, seg, 0), n, W));
+  const int i1 = uniform(owner(base + place_of(en, seg, en.units - 1), n, W));
   if (i0 == i1) return;                            // one workgroup had it all, and wrote it
 
   auto slot = [&](int i) { return 2 * i + (i == i0 ? 1 : 0); };   // i0's run holds the segment's first unit
@@ -141,7 +142,7 @@ CacheAttnShape cache_attn_shape(const CacheAttnArgs& a) {
   // as many workgroups as are resident at once
   const int resident = kCus * (s.shared ? 2 : wave_residents(a.c.D, s.tiles));
   const int cap = a.max_pages << a.c.log2_page;
-  const Entry e = entry_of(cap, a.T, cap, a.T, a.G, 16 * s.tiles, true, true);
+  const Entry e = entry_of(cap, a.T, cap, a.T, a.G, 16 * s.tiles, true, 0);
   s.split = e.units > kWholeUnits;
   const int64_t most = (int64_t)(s.split ? e.units : 1) * e.tiles * a.c.heads * a.B;
   s.wgs = (int)(most < resident ? most : resident);

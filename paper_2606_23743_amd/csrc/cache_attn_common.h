@@ -63,15 +63,15 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// units of all segments, and the entry that unit x falls into with its first unit; by one wave
+// places of all segments, and the entry that place x falls into with its first place; by one wave
 struct Finder {
   const CacheAttnArgs& a;
-  int rows;
+  int rows, begin;
   int64_t incl;                  // B <= 64: the scan of the only chunk
   int64_t total;
 
   __device__ __forceinline__ Entry of(int len, int cnt) const {
-    return entry_of(len, cnt, a.max_pages << a.c.log2_page, a.T, a.G, rows, a.kn.p != nullptr, a.divide);
+    return entry_of(len, cnt, a.max_pages << a.c.log2_page, a.T, a.G, rows, a.kn.p != nullptr, begin);
   }
   // b alike in all lanes
   __device__ __forceinline__ Entry at(int b) const {
@@ -87,11 +87,19 @@ struct Finder {
     }
     return x;
   }
-  __device__ __forceinline__ Finder(const CacheAttnArgs& args, int rows_) : a(args), rows(rows_) {
+  __device__ __forceinline__ void sum() {
     total = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
       incl = scan(b0);
       total += uniform(__shfl(incl, 63));
+    }
+  }
+  __device__ __forceinline__ Finder(const CacheAttnArgs& args, int rows_, int grid)
+      : a(args), rows(rows_), begin(args.divide ? 0 : -1) {
+    sum();
+    if (a.divide && begin_of(total, grid) > 0) {
+      begin = begin_of(total, grid);
+      sum();
     }
   }
   // x < total

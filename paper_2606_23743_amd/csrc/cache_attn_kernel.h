@@ -175,17 +175,17 @@ void cache_attn_kernel(CacheAttnArgs a) {
   const int log2p = a.c.log2_page, pmask = (1 << log2p) - 1;
   const int Hkv = a.c.heads;
 
-  const Finder fd(a, RPT);
-  const int64_t U = fd.total;
-  if (U == 0) return;
-  const int n = (int)min((int64_t)gridDim.x, U);
+  const Finder fd(a, RPT, gridDim.x);
+  const int64_t W = fd.total;
+  if (W == 0) return;
+  const int n = (int)min((int64_t)gridDim.x, W);
   // neighbouring runs on one XCD where row tiles of a head read the same keys; a grid
   // with workgroups to spare spreads over all XCDs instead
   const int me = a.G * a.T > RPT && n == (int)gridDim.x ? xcd_remap(blockIdx.x, n) : blockIdx.x;
   if (me >= n) return;
-  int64_t x = uniform(first_unit(me, n, U));
-  const int64_t end = uniform(first_unit(me + 1, n, U));
-  int64_t ebase;                                   // first unit of entry b
+  int64_t x = uniform(run_of(me, n, W));
+  const int64_t end = uniform(run_of(me + 1, n, W));
+  int64_t ebase;                                   // first place of entry b
   int b = fd.find(x, ebase);
 
   while (x < end) {
@@ -196,11 +196,11 @@ void cache_attn_kernel(CacheAttnArgs a) {
       ++b;
       continue;
     }
-    const int seg = uniform((int)div_floor(x - ebase, en.span));
-    const int u0 = (int)(x - ebase - (int64_t)seg * en.span);
-    const int u1 = a.divide ? (int)min((int64_t)en.units, u0 + (end - x)) : en.units;
+    const Piece pc = piece_at(en, x - ebase, end - x);
+    const int seg = uniform(pc.seg), u0 = uniform(pc.u0), u1 = uniform(pc.u1);
+    x = ebase + uniform(pc.next);
+    if (u0 >= u1) continue;
     const int h = uniform(seg / en.tiles), rt = seg - h * en.tiles;
-    x += a.divide ? u1 - u0 : 1;
 
     // the token and head of the lane's column in tile qt; token -1: no such row
     auto row_of = [&](int qt, int& tok, int& head) {
