@@ -29,14 +29,14 @@ __global__ __launch_bounds__(64 * kJoinGroups) void cache_join_kernel(CacheAttnA
   const int h = id % a.c.heads, b = id / a.c.heads;
 
   const Finder fd(a, RPT, grid_n);
-  const Entry en = fd.at(b);
+  const Entry en = fd.kept(b);
   if (rt >= en.tiles || (rt * RPT + qt * 16) >= en.cnt * a.G) return;
   const int64_t W = fd.total;
   const int n = (int)min((int64_t)grid_n, W);
   // the entry's first place: the scan up to b
   int64_t base = 0;
   for (int b0 = 0; b0 < b; b0 += 64) {
-    const int64_t in = a.B <= 64 ? fd.incl : fd.scan(b0);
+    const int64_t in = b0 == 0 ? fd.incl : fd.scan(b0);
     base += uniform(__shfl(in, min(b - b0, 64) - 1));
   }
   const int64_t seg = (int64_t)h * en.tiles + rt;

@@ -67,7 +67,8 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 struct Finder {
   const CacheAttnArgs& a;
   int rows, begin;
-  int64_t incl;                  // B <= 64: the scan of the only chunk
+  int len0, cnt0;                // the lane's entry of the first 64
+  int64_t incl;                  // the scan of the first 64 entries
   int64_t total;
 
   __device__ __forceinline__ Entry of(int len, int cnt) const {
@@ -77,9 +78,15 @@ struct Finder {
   __device__ __forceinline__ Entry at(int b) const {
     return of(uniform(a.lens[b]), a.counts ? uniform(a.counts[b]) : a.T);
   }
-  __device__ __forceinline__ int64_t scan(int b0) const {
-    const int b = b0 + (int)(threadIdx.x & 63);
-    int64_t x = b < a.B ? entry_work(of(a.lens[b], a.counts ? a.counts[b] : a.T), a.c.heads) : 0;
+  // the same without another look at memory where b is one of the first 64
+  __device__ __forceinline__ Entry kept(int b) const {
+    if (b >= 64) return at(b);
+    return of(__builtin_amdgcn_readlane(len0, b), __builtin_amdgcn_readlane(cnt0, b));
+  }
+  __device__ __forceinline__ int len_at(int b) const { return b < a.B ? a.lens[b] : 0; }
+  __device__ __forceinline__ int cnt_at(int b) const { return b < a.B && a.counts ? a.counts[b] : a.T; }
+  __device__ __forceinline__ int64_t scan(int b, int len, int cnt) const {
+    int64_t x = b < a.B ? entry_work(of(len, cnt), a.c.heads) : 0;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const int64_t y = __shfl_up(x, d);
@@ -87,15 +94,19 @@ struct Finder {
     }
     return x;
   }
+  __device__ __forceinline__ int64_t scan(int b0) const {
+    const int b = b0 + (int)(threadIdx.x & 63);
+    return scan(b, len_at(b), cnt_at(b));
+  }
   __device__ __forceinline__ void sum() {
-    total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-      incl = scan(b0);
-      total += uniform(__shfl(incl, 63));
-    }
+    incl = scan(threadIdx.x & 63, len0, cnt0);
+    total = uniform(__shfl(incl, 63));
+    for (int b0 = 64; b0 < a.B; b0 += 64) total += uniform(__shfl(scan(b0), 63));
   }
   __device__ __forceinline__ Finder(const CacheAttnArgs& args, int rows_, int grid)
       : a(args), rows(rows_), begin(args.divide ? 0 : -1) {
+    len0 = len_at(threadIdx.x & 63);
+    cnt0 = cnt_at(threadIdx.x & 63);
     sum();
     if (a.divide && begin_of(total, grid) > 0) {
       begin = begin_of(total, grid);
@@ -106,7 +117,7 @@ struct Finder {
   __device__ __forceinline__ int find(int64_t x, int64_t& first) const {
     int64_t base = 0;
     for (int b0 = 0;; b0 += 64) {
-      const int64_t in = a.B <= 64 ? incl : scan(b0);
+      const int64_t in = b0 == 0 ? incl : scan(b0);
       const uint64_t past = __builtin_amdgcn_ballot_w64(base + in > x);
       if (past != 0) {
         const int k = __builtin_ctzll(past);

@@ -188,12 +188,12 @@ void cache_attn_kernel(CacheAttnArgs a) {
   int64_t ebase;                                   // first place of entry b
   int b = fd.find(x, ebase);
 
+  Entry en = fd.kept(b);
   while (x < end) {
-    const Entry en = fd.at(b);
     const int64_t work = entry_work(en, Hkv);
     if (x >= ebase + work) {                       // the next entry
       ebase += work;
-      ++b;
+      en = fd.at(++b);
       continue;
     }
     const Piece pc = piece_at(en, x - ebase, end - x);
@@ -208,6 +208,20 @@ void cache_attn_kernel(CacheAttnArgs a) {
       tok = t < en.cnt ? t : -1;
       head = h * a.G + (row - t * a.G);
     };
+    // ---- the first step's pages: nothing waits for Q before its keys are on their way ----
+    const int32_t* table = a.table + (int64_t)b * a.max_pages;
+    const int kq = 8 * (i16 >> 2), kv8 = 8 * g;    // this lane's K rows and V rows of a step begin here
+    auto page_at = [&](int key) { return table[min(key >> log2p, a.max_pages - 1)]; };
+    // this wave's steps: units u0 .. ulast - 1 of which its 32 keys begin before the end
+    int ulast = min(u1, en.cached_units);
+    if (ulast > u0 && (ulast - 1) * kUnit + 32 * w >= en.len) --ulast;
+    int pk = 0, pv = 0;
+    auto load_pages = [&](int u) {
+      pk = page_at(u * kUnit + 32 * w + kq);
+      pv = page_at(u * kUnit + 32 * w + kv8);
+    };
+    if (u0 < ulast) load_pages(u0);
+
     // ---- Q of this tile's rows ----
     auto load_q = [&](int qt, int s) {
       int t, head;
@@ -221,12 +235,7 @@ void cache_attn_kernel(CacheAttnArgs a) {
     bf16x8 q1[KS];                                 // one tile stays in registers, more lie in LDS
     if constexpr (QT == 1) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        q1[s] = __builtin_bit_cast(bf16x8, load_q(0, s));
-        // it has landed here: without this use the compiler waits for it again in every step,
-        // and with it for the codes that are on their way
-        asm volatile("" : "+v"(q1[s]));
-      }
+      for (int s = 0; s < KS; ++s) q1[s] = __builtin_bit_cast(bf16x8, load_q(0, s));
     } else {
 #pragma unroll 1
       for (int qt = w; qt < QT; qt += kWaves)
@@ -255,17 +264,6 @@ void cache_attn_kernel(CacheAttnArgs a) {
     };
 
     // ---- cached keys ----
-    const int32_t* table = a.table + (int64_t)b * a.max_pages;
-    const int kq = 8 * (i16 >> 2), kv8 = 8 * g;    // this lane's K rows and V rows of a step begin here
-    auto page_at = [&](int key) { return table[min(key >> log2p, a.max_pages - 1)]; };
-    // this wave's steps: units u0 .. ulast - 1 of which its 32 keys begin before the end
-    int ulast = min(u1, en.cached_units);
-    if (ulast > u0 && (ulast - 1) * kUnit + 32 * w >= en.len) --ulast;
-    int pk = 0, pv = 0;
-    auto load_pages = [&](int u) {
-      pk = page_at(u * kUnit + 32 * w + kq);
-      pv = page_at(u * kUnit + 32 * w + kv8);
-    };
     // K and its scales, with the pages loaded for it; the next page numbers go out first, so
     // that waiting for them waits for nothing else
     auto load_k = [&](Raw<FMT, D>& r, int u) {
@@ -394,9 +392,14 @@ void cache_attn_kernel(CacheAttnArgs a) {
     };
     if (u0 < ulast) {
       Raw<FMT, D> r;
-      load_pages(u0);
       load_k(r, u0);
       load_v(r);
+      // Q has landed here: without this use the compiler waits for it again in every step,
+      // and with it for the codes that are on their way
+      if constexpr (QT == 1) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q1[s]));
+      }
       for (int u = u0; u < ulast; ++u) work_on(r, u);
     }
 

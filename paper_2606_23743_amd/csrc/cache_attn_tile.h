@@ -68,12 +68,12 @@ void cache_tile_kernel(CacheAttnArgs a) {
   attn::operand_offsets16<D>(lane, koff, voff);
   const int srow = threadIdx.x / LPR, piece = threadIdx.x % LPR;
 
+  Entry en = fd.kept(b);
   while (x < end) {
-    const Entry en = fd.at(b);
     const int64_t work = entry_work(en, Hkv);
     if (x >= ebase + work) {
       ebase += work;
-      ++b;
+      en = fd.at(++b);
       continue;
     }
     const Piece pc = piece_at(en, x - ebase, end - x);
