@@ -37,7 +37,7 @@ __global__ __launch_bounds__(64 * kJoinGroups) void cache_join_kernel(CacheAttnA
   int64_t base = 0;
   for (int b0 = 0; b0 < b; b0 += 64) {
     const int64_t in = b0 == 0 ? fd.incl : fd.scan(b0);
-    base += uniform(__shfl(in, min(b - b0, 64) - 1));
+    base += lane_value(in, min(b - b0, 64) - 1);
   }
   const int64_t seg = (int64_t)h * en.tiles + rt;
   const int i0 = uniform(owner(base + place_of(en, seg, 0), n, W));

@@ -63,6 +63,29 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// lane l's value
+__device__ __forceinline__ int64_t lane_value(int64_t x, int l) {
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, l), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), l);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// sums over lanes 0 .. l, in each lane l (DPP: within rows of 16 lanes, then a row's last
+// lane to the next row, then lane 31 to the upper half)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t moved(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+  x += moved<0x111, 0xf>(x);
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);
+  x += moved<0x143, 0xc>(x);
+  return x;
+}
+
 // places of all segments, and the entry that place x falls into with its first place; by one wave
 struct Finder {
   const CacheAttnArgs& a;
@@ -86,13 +109,7 @@ struct Finder {
   __device__ __forceinline__ int len_at(int b) const { return b < a.B ? a.lens[b] : 0; }
   __device__ __forceinline__ int cnt_at(int b) const { return b < a.B && a.counts ? a.counts[b] : a.T; }
   __device__ __forceinline__ int64_t scan(int b, int len, int cnt) const {
-    int64_t x = b < a.B ? entry_work(of(len, cnt), a.c.heads) : 0;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t y = __shfl_up(x, d);
-      if ((int)(threadIdx.x & 63) >= d) x += y;
-    }
-    return x;
+    return wave_scan(b < a.B ? entry_work(of(len, cnt), a.c.heads) : 0);
   }
   __device__ __forceinline__ int64_t scan(int b0) const {
     const int b = b0 + (int)(threadIdx.x & 63);
@@ -100,8 +117,8 @@ struct Finder {
   }
   __device__ __forceinline__ void sum() {
     incl = scan(threadIdx.x & 63, len0, cnt0);
-    total = uniform(__shfl(incl, 63));
-    for (int b0 = 64; b0 < a.B; b0 += 64) total += uniform(__shfl(scan(b0), 63));
+    total = lane_value(incl, 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64) total += lane_value(scan(b0), 63);
   }
   __device__ __forceinline__ Finder(const CacheAttnArgs& args, int rows_, int grid)
       : a(args), rows(rows_), begin(args.divide ? 0 : -1) {
@@ -121,10 +138,10 @@ struct Finder {
       const uint64_t past = __builtin_amdgcn_ballot_w64(base + in > x);
       if (past != 0) {
         const int k = __builtin_ctzll(past);
-        first = base + (k > 0 ? uniform(__shfl(in, k > 0 ? k - 1 : 0)) : 0);
+        first = base + (k > 0 ? lane_value(in, k > 0 ? k - 1 : 0) : 0);
         return b0 + k;
       }
-      base += uniform(__shfl(in, 63));
+      base += lane_value(in, 63);
     }
   }
 };

@@ -25,7 +25,7 @@ namespace cattn {
 constexpr int kUnit = 128;       // keys of a unit
 // Segments of at most so many units are not divided: the join's launch takes longer than the
 // units one after the other (us a call, divided / whole, 8 cache heads of 500 tokens: one
-// sequence 18.4 / 15.8, 64 of them 27.4 / 20.9; 16 of 900 tokens 19.9 / 21.4, one of 1,900
+// sequence 18.4 / 15.6, 64 of them 25.7 / 19.7; 16 of 900 tokens 19.9 / 21.4, one of 1,900
 // 17.6 / 30.6)
 constexpr int kWholeUnits = 6;
 constexpr int kWaves = 4;
