@@ -5,12 +5,13 @@
 // alone in place.
 //
 // Bound by HBM: an element is read and written once and costs two products.
-// One workgroup takes a few tokens with all heads of Q and K, because a pair's
+// One workgroup takes a few tokens with all heads of Q and K (or several of them, where
+// a head's tokens lie together), because a pair's
 // angle is the same in every head: it first tabulates (m cos t, m sin t) of its
 // tokens in LDS (the angle reduced modulo one turn in float64, so that positions
 // of a million are as exact as small ones), then streams rows, 16 bytes an
 // access, a lane's three to six items in flight together.  63,240 tokens of 40 heads of 128, half
-// of each turned: 220 us, 5.9 TB/s.
+// of each turned: 222 us, 5.8 TB/s; 2 x 7,801 float32 tokens of 40 heads of 112: 97 us, 5.8 TB/s.
 #include "sva_internal.h"
 
 namespace sva {
@@ -25,7 +26,8 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 struct RotaryGrid {
-  int tok;                       // tokens of a workgroup
+  int tok, heads;                // tokens and heads of a workgroup
+  bool by_head;                  // its items in the order (head, token) instead of (token, head): BY_HEAD
   int rot_items, row_items;      // items of a row that turn, and all of them
 };
 
@@ -81,7 +83,7 @@ template <> struct Elem<true> {
   }
 };
 
-template <bool F32, bool HALF, bool VEC, int kUnroll, bool NT>
+template <bool F32, bool HALF, bool VEC, int kUnroll, bool NT, bool BY_HEAD>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGrid gr) {
   using El = Elem<F32>;
   using T = typename El::T;
@@ -111,8 +113,10 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
   }
   __syncthreads();
 
-  const int heads = a.qi.heads + a.ki.heads;
+  const int h0 = BY_HEAD ? blockIdx.y * gr.heads : 0;
+  const int all = a.qi.heads + a.ki.heads, heads = BY_HEAD ? min(gr.heads, all - h0) : all;
   const int items = nt * heads * gr.row_items;
+  const unsigned inner = BY_HEAD ? nt : heads;
   for (int i0 = 0; i0 < items; i0 += kThreads * kUnroll) {
     const T* src[kUnroll];
     T* dst[kUnroll];
@@ -124,8 +128,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
       const unsigned idx = min(i0 + u * kThreads + (int)threadIdx.x, items - 1);
       const unsigned row = idx / (unsigned)gr.row_items;
       c[u] = idx - row * gr.row_items;
-      const unsigned tk = row / (unsigned)heads;
-      const int h = row - tk * heads;
+      const unsigned far = row / inner, near = row - far * inner;
+      const unsigned tk = BY_HEAD ? near : far;
+      const int h = h0 + (int)(BY_HEAD ? far : near);
       const bool isq = h < a.qi.heads;
       const int hh = isq ? h : h - a.qi.heads;
       src[u] = (const T*)(isq ? a.qi.p : a.ki.p) + base[tk][isq ? 0 : 2] + hh * (isq ? a.qi.sh : a.ki.sh);
@@ -197,18 +202,36 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
 template <bool F32, bool HALF, bool VEC, int U>
 void launch_unroll(const RotaryArgs& a, const RotaryGrid& gr, bool nt, hipStream_t stream) {
   const int64_t tokens = (int64_t)a.B * a.N;
-  const dim3 grid((unsigned)((tokens + gr.tok - 1) / gr.tok));
-  if (nt) hipLaunchKernelGGL((rotary_kernel<F32, HALF, VEC, U, VEC>), grid, dim3(kThreads), 0, stream, a, gr);
-  else hipLaunchKernelGGL((rotary_kernel<F32, HALF, VEC, U, false>), grid, dim3(kThreads), 0, stream, a, gr);
+  const int heads = a.qi.heads + a.ki.heads;
+  const dim3 grid((unsigned)((tokens + gr.tok - 1) / gr.tok), (heads + gr.heads - 1) / gr.heads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a, gr); };
+  if (gr.by_head && nt) go(rotary_kernel<F32, HALF, VEC, U, VEC, true>);
+  else if (gr.by_head) go(rotary_kernel<F32, HALF, VEC, U, false, true>);
+  else if (nt) go(rotary_kernel<F32, HALF, VEC, U, VEC, false>);
+  else go(rotary_kernel<F32, HALF, VEC, U, false, false>);
 }
 
 template <bool F32, bool HALF, bool VEC>
 void launch_as(const RotaryArgs& a, hipStream_t stream) {
   constexpr int E = VEC ? Elem<F32>::E : 1, kItem = F32 ? 4 : 2;
-  RotaryGrid gr{1, 0, 0};
+  const int heads = a.qi.heads + a.ki.heads;
+  RotaryGrid gr{1, heads, false, 0, 0};
   gr.rot_items = !VEC || HALF ? a.rot / 2 / E : a.rot / E;
   gr.row_items = gr.rot_items + (a.copy ? (a.D - a.rot) / E : 0);
-  const int64_t per_token = (int64_t)(a.qi.heads + a.ki.heads) * gr.row_items;
+  // Where a head's tokens lie together (not a token's heads), a workgroup takes 4 KB of each of
+  // as many heads as make four items a lane; us against all heads of fewer tokens, 2 x 7,801
+  // tokens of 40 heads of 112: float32 115 / 97, bf16 interleaved 85 / 57, halves 61 / 52;
+  // 30,000 tokens of 40 of 128 119 / 109, of 64 61 / 57
+  if (a.N > 1 && a.qi.sn < a.qi.sh && heads <= 65535) {   // (groups are blockIdx.y)
+    int64_t t = 4096 / (a.D * kItem);
+    t = t < kMaxTok ? (t > 1 ? t : 1) : kMaxTok;
+    int64_t most = 4 * kThreads / (t * gr.row_items);
+    if (most < 1) most = 1;
+    const int64_t groups = (heads + most - 1) / most;
+    gr.heads = (int)((heads + groups - 1) / groups);
+    gr.by_head = true;
+  }
+  const int64_t per_token = (int64_t)gr.heads * gr.row_items;
   // Tokens of a workgroup, within the table, and items of a lane: one round of the lanes, or
   // as few as the heads of one token need, with the fewest lanes idle.  More rounds were
   // slower: 63,240 tokens of 40 heads of 128, half turned, 220 us in one, 262 in four.

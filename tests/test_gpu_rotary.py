@@ -93,6 +93,18 @@ def test_sizes(B, H, Hk, N):
     _case(B, H, Hk, N, 128, 128, "half", "bf16")
 
 
+@pytest.mark.parametrize("dtype,layout", itertools.product(["bf16", "f32"], ["half", "interleaved"]))
+@pytest.mark.parametrize("B,H,Hk,N,D,rot", [(2, 33, 8, 45, 112, 112), (1, 40, 1, 130, 64, 64), (3, 7, 12, 50, 256, 96),
+                                            (1, 65, 0, 17, 66, 34)])
+def test_heads_are_divided_where_a_heads_tokens_lie_together(B, H, Hk, N, D, rot, dtype, layout):
+    for in_place in (False, True):
+        _case(B, H, Hk, N, D, rot, layout, dtype, in_place=in_place)
+
+
+def test_more_heads_than_groups_may_be():
+    _case(1, 66000, 1, 2, 64, 64, "half", "bf16")
+
+
 def test_misaligned_pointer_takes_the_general_path():
     _case(1, 3, 2, 11, 128, 128, "half", "bf16", offset=1)
     _case(1, 3, 2, 11, 128, 64, "interleaved", "f32", offset=1)
