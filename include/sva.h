@@ -516,8 +516,8 @@ typedef struct sva_cache {
  *   dtype : sva_dtype of k and v ([B, Hkv, N, D]; 16-byte aligned data and strides)
  *   slots : int32 device, token (b, n) goes to slots[b * slots_stride_b + n]; a
  *           value outside [0, num_pages * page_size) writes nothing (padding,
- *           rejected drafts).  The others must differ from each other: where
- *           two tokens name one slot its codes and scale may be of either.
+ *           rejected drafts).  The others must differ from each other: a slot
+ *           that two tokens name is left with a mix of both.
  * Slots that are not named keep their contents. */
 int sva_cache_write(const sva_cache* cache, int32_t batch, int32_t tokens, int32_t dtype,
                     const sva_heads* k, const sva_heads* v, const int32_t* slots,
@@ -569,8 +569,8 @@ int sva_cache_attention_workspace(const sva_cache* cache, const sva_cache_query*
  *   counts     : int32 [B] device or NULL: the drafted tokens that entry b has,
  *                clamped to [0, T]; those behind it are neither keys nor
  *                queries, and their rows of out and lse are left as they were
- *   out        : [B, H, T, D], bf16 or float32; zeros for a query that attends
- *                to nothing
+ *   out        : [B, H, T, D], bf16 or float32, apart from every input; zeros
+ *                for a query that attends to nothing
  *   lse        : float32 [B, H, T] contiguous or NULL; natural-log log-sum-exp of
  *                the scaled logits (-inf for a query that attends to nothing)
  *   workspace  : device memory, 256-byte aligned, at least
@@ -582,7 +582,7 @@ int sva_cache_attention_workspace(const sva_cache* cache, const sva_cache_query*
  * and multiplied by bf16 MFMA with float32 accumulation, the scales applied to
  * logits and weights in float32, with a running maximum.  For a bf16 result
  * the weights are rounded to bf16 before the product with V; for a float32
- * result they are carried as a sum of two bf16 values.  The keys of all
+ * result they are carried as a sum of three bf16 values.  The keys of all
  * sequences are divided evenly among workgroups, so the order in which a
  * query's partial results are added, and with it its last bits, depends on the
  * lengths in the call; the same call gives the same bits. */

@@ -86,62 +86,101 @@ __device__ __forceinline__ int64_t wave_scan(int64_t x) {
   return x;
 }
 
-// places of all segments, and the entry that place x falls into with its first place; by one wave
+// Places of all segments, and the entry that holds a place, by one wave.  Each lane sums
+// B / 64 neighbouring entries, one scan over the lanes gives every lane's first place, and the
+// lane that holds what is looked for is taken apart in the same way (up to 64 entries: one
+// look at memory in all; 4,096: two).
 struct Finder {
   const CacheAttnArgs& a;
   int rows, begin;
-  int len0, cnt0;                // the lane's entry of the first 64
-  int64_t incl;                  // the scan of the first 64 entries
+  int per;                       // entries of a lane
+  int len0, cnt0;                // per = 1: the lane's entry
+  int64_t incl;                  // places of this lane's entries and all before them
   int64_t total;
 
   __device__ __forceinline__ Entry of(int len, int cnt) const {
     return entry_of(len, cnt, a.max_pages << a.c.log2_page, a.T, a.G, rows, a.kn.p != nullptr, begin);
   }
   // b alike in all lanes
-  __device__ __forceinline__ Entry at(int b) const {
-    return of(uniform(a.lens[b]), a.counts ? uniform(a.counts[b]) : a.T);
+  __device__ __forceinline__ Entry at(int b) const { return of(uniform(len_at(b)), uniform(cnt_at(b))); }
+  __device__ __forceinline__ int len_at(int b) const { return a.lens[min(b, a.B - 1)]; }
+  __device__ __forceinline__ int cnt_at(int b) const { return a.counts ? a.counts[min(b, a.B - 1)] : a.T; }
+
+  // units and segments of n entries from b on
+  struct Sums {
+    int64_t units, segments;
+  };
+  __device__ __forceinline__ Sums one(int len, int cnt) const {
+    const Entry e = of(len, cnt);
+    const int64_t s = (int64_t)e.tiles * a.c.heads;
+    return {e.units * s, s};
   }
-  // the same without another look at memory where b is one of the first 64
-  __device__ __forceinline__ Entry kept(int b) const {
-    if (b >= 64) return at(b);
-    return of(__builtin_amdgcn_readlane(len0, b), __builtin_amdgcn_readlane(cnt0, b));
+  __device__ __forceinline__ Sums sums(int b, int n) const {
+    Sums x{0, 0};
+    constexpr int UN = 8;                          // loads on their way together
+    for (int j = 0; j < n; j += UN) {
+      int len[UN], cnt[UN];
+#pragma unroll
+      for (int k = 0; k < UN; ++k) {
+        len[k] = len_at(b + j + k);
+        cnt[k] = cnt_at(b + j + k);
+      }
+#pragma unroll
+      for (int k = 0; k < UN; ++k) {
+        const Sums y = one(len[k], cnt[k]);
+        x.units += j + k < n ? y.units : 0;
+        x.segments += j + k < n ? y.segments : 0;
+      }
+    }
+    return x;
   }
-  __device__ __forceinline__ int len_at(int b) const { return b < a.B ? a.lens[b] : 0; }
-  __device__ __forceinline__ int cnt_at(int b) const { return b < a.B && a.counts ? a.counts[b] : a.T; }
-  __device__ __forceinline__ int64_t scan(int b, int len, int cnt) const {
-    return wave_scan(b < a.B ? entry_work(of(len, cnt), a.c.heads) : 0);
-  }
-  __device__ __forceinline__ int64_t scan(int b0) const {
-    const int b = b0 + (int)(threadIdx.x & 63);
-    return scan(b, len_at(b), cnt_at(b));
-  }
-  __device__ __forceinline__ void sum() {
-    incl = scan(threadIdx.x & 63, len0, cnt0);
-    total = lane_value(incl, 63);
-    for (int b0 = 64; b0 < a.B; b0 += 64) total += lane_value(scan(b0), 63);
-  }
+  __device__ __forceinline__ int64_t places(Sums s) const { return begin < 0 ? s.segments : s.units + begin * s.segments; }
+
   __device__ __forceinline__ Finder(const CacheAttnArgs& args, int rows_, int grid)
-      : a(args), rows(rows_), begin(args.divide ? 0 : -1) {
-    len0 = len_at(threadIdx.x & 63);
-    cnt0 = cnt_at(threadIdx.x & 63);
-    sum();
+      : a(args), rows(rows_), begin(args.divide ? 0 : -1), per((args.B + 63) >> 6), len0(0), cnt0(0) {
+    const int lane = threadIdx.x & 63, n = min(max(a.B - lane * per, 0), per);
+    Sums s{0, 0};
+    if (per == 1) {
+      len0 = len_at(lane);
+      cnt0 = cnt_at(lane);
+      const Sums y = one(len0, cnt0);
+      if (n > 0) s = y;
+    } else {
+      s = sums(lane * per, n);
+    }
+    incl = wave_scan(places(s));
+    total = lane_value(incl, 63);
     if (a.divide && begin_of(total, grid) > 0) {
       begin = begin_of(total, grid);
-      sum();
+      incl += begin * wave_scan(s.segments);
+      total = lane_value(incl, 63);
     }
   }
-  // x < total
-  __device__ __forceinline__ int find(int64_t x, int64_t& first) const {
-    int64_t base = 0;
-    for (int b0 = 0;; b0 += 64) {
-      const int64_t in = b0 == 0 ? incl : scan(b0);
-      const uint64_t past = __builtin_amdgcn_ballot_w64(base + in > x);
-      if (past != 0) {
-        const int k = __builtin_ctzll(past);
-        first = base + (k > 0 ? lane_value(in, k > 0 ? k - 1 : 0) : 0);
-        return b0 + k;
+
+  // the entry that holds place x < total, or (want >= 0) entry want; which it is and its first place
+  __device__ __forceinline__ Entry locate(int64_t x, int want, int& b, int64_t& first) const {
+    const int lane = threadIdx.x & 63;
+    int64_t in = incl;
+    int lo = 0, each = per, len = len0, cnt = cnt0;
+    first = 0;
+    for (;;) {
+      const int k = want >= 0 ? (want - lo) / each : __builtin_ctzll(__builtin_amdgcn_ballot_w64(first + in > x));
+      if (k > 0) first += lane_value(in, k - 1);
+      lo += k * each;
+      if (each == 1) {
+        b = lo;
+        return of(__builtin_amdgcn_readlane(len, k), __builtin_amdgcn_readlane(cnt, k));
       }
-      base += lane_value(in, 63);
+      const int n = min(each, a.B - lo);
+      each = (n + 63) >> 6;
+      const int m = min(max(n - lane * each, 0), each);
+      if (each == 1) {
+        len = len_at(lo + lane);
+        cnt = cnt_at(lo + lane);
+        in = wave_scan(m > 0 ? places(one(len, cnt)) : 0);
+      } else {
+        in = wave_scan(places(sums(lo + lane * each, m)));
+      }
     }
   }
 };

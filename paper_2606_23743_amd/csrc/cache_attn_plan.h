@@ -6,14 +6,14 @@
 // units of 128 (a 32-key step of each of four waves): first the cached keys,
 // then the drafted ones, at least one unit.  The units of all segments, in the
 // order (entry, head, tile, key), are dealt to n workgroups in runs of equal
-// length.  Units have places: one each, and where runs are long a segment's first unit takes
-// kBegin more, for what beginning a segment costs; workgroup i takes the units whose places
-// begin in [i*W/n, (i+1)*W/n) of W.  However ragged the lengths, every workgroup then has the
-// same work; a run may cross segments, and a segment whose units went to several workgroups is joined from
-// their partial results afterwards.  Short caches are not divided (their segments count as
-// one unit each): joining would cost more than it gives.  A workgroup leaves at most two parts:
-// slot 2i for a run that begins inside a segment, 2i + 1 for one that begins with a
-// segment and ends inside it.
+// length: units have places (one each; where runs are long a segment's first takes
+// kBegin more, for what beginning a segment costs), and workgroup i takes the units
+// whose places begin in [i*W/n, (i+1)*W/n) of W.  However ragged the lengths, every
+// workgroup then has the same work; a run may cross segments, and a segment whose
+// units went to several workgroups is joined from their partial results afterwards.
+// Short caches are not divided (their segments count as one unit each): joining would
+// cost more than it gives.  A workgroup leaves at most two parts: slot 2i for a run that
+// begins inside a segment, 2i + 1 for one that begins with a segment and ends inside it.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -56,7 +56,7 @@ __host__ __device__ __forceinline__ Entry entry_of(int len, int cnt, int max_len
   e.cached_units = (int)(((int64_t)e.len + kUnit - 1) / kUnit);
   e.units = e.cached_units + (drafts ? (e.cnt + kUnit - 1) / kUnit : 0);
   if (e.units < 1) e.units = 1;
-  e.tiles = (int)(((int64_t)e.cnt * G + rows - 1) / rows);
+  e.tiles = (e.cnt * G + rows - 1) / rows;   // (cnt <= 1,024, G <= 65,536)
   e.begin = begin;
   e.span = begin < 0 ? 1 : e.units + begin;
   return e;

@@ -1,8 +1,10 @@
 // Attention of drafted tokens over a paged cache for many query rows per cache head
-// (trees; cache_attn_kernel.h has the form for few).
+// (trees; cache_attn_kernel.h has the form for up to 48).
 //
 // What bounds it: from about 64 rows on a code that is read once meets enough rows
-// that widening it, the softmax and the products take longer than reading it, and
+// that widening it, the softmax and the products take longer than reading it (8 ragged
+// sequences of up to 75,600 int8 tokens, 6 heads of 128, up to 192 rows: 186 MB and 69 GFLOP in
+// 105 us, 660 TFLOP/s), and
 // if every wave widened its own keys, widening would come before the products.  So
 // the workgroup's four waves own QT tiles of 16 rows each and share the keys: 64 at
 // a time are widened once, by all lanes together, into row-major bf16 tiles in LDS
@@ -11,10 +13,9 @@
 // of the 64 after them.  Two stages, one barrier per 64 keys, and no meeting of the
 // waves at the end: each has whole rows.
 //
-// The softmax keeps the running maximum of cache_attn_kernel.h, but looks at the sums
-// of a step's weights instead of the logits: only where one exceeds 2^10 (or the row is
-// new) is the step's maximum taken and the reference moved, so a weight costs one fma,
-// one exponential and one addition.
+// The softmax keeps the running maximum of cache_attn_kernel.h: only where the sum of a
+// step's weights exceeds 2^10 (or the row is new) is the step's maximum taken and the
+// reference moved, so a weight costs one fma, one exponential and one addition.
 #pragma once
 
 #include "cache_attn_common.h"
@@ -62,13 +63,13 @@ void cache_tile_kernel(CacheAttnArgs a) {
   int64_t x = uniform(run_of(me, n, W));
   const int64_t end = uniform(run_of(me + 1, n, W));
   int64_t ebase;
-  int b = fd.find(x, ebase);
+  int b;
 
   int koff[G16::KS], voff[G16::DT];
   attn::operand_offsets16<D>(lane, koff, voff);
   const int srow = threadIdx.x / LPR, piece = threadIdx.x % LPR;
 
-  Entry en = fd.kept(b);
+  Entry en = fd.locate(x, -1, b, ebase);
   while (x < end) {
     const int64_t work = entry_work(en, Hkv);
     if (x >= ebase + work) {

@@ -206,6 +206,33 @@ def test_many_sequences():
     c.run(mask=trees(c.g, 150, 2))
 
 
+@pytest.mark.parametrize("B,kv,T", [(63, 9, 2), (64, 8, 1), (65, 1, 3), (200, 3, 1), (1025, 1, 2), (4097, 1, 1), (4200, 2, 1)])
+@pytest.mark.parametrize("long", [False, True])
+def test_batches_that_lanes_and_their_entries_divide(B, kv, T, long):
+    """Pages shared by entries; lengths short but for a few, counts of zero among them."""
+    c = Case.__new__(Case)
+    g = c.g = np.random.default_rng(B + long)
+    c.B, c.kv, c.T, c.D, c.page = B, kv, T, 64, 64
+    c.lengths = g.integers(0, 40, B)
+    if long:
+        c.lengths[g.choice(B, 12, replace=False)] = g.integers(300, 2500, 12)
+        c.lengths[[0, B - 1]] = 1500, 2300
+    columns = 40 if long else 5
+    c.host, c.values = host_cache(g, 90, kv, 64, 64, "e4m3")
+    c.table = g.integers(0, 90, (B, columns)).astype(np.int32)
+    c.q, c.k_new, c.v_new = bf16_normal(g, (B, 2 * kv, T, 64), 1.5), bf16_normal(g, (B, kv, T, 64)), bf16_normal(g, (B, kv, T, 64))
+    say(f"[cache attention] B={B} kv={kv} T={T} long={long}")
+    c.run()
+    counts = g.integers(0, T + 1, B)
+    counts[[0, B - 1]] = 1, T
+    out, lse = c.call(counts=counts, out=torch.full((B, 2 * kv, T, 64), 7.0, dtype=torch.bfloat16, device="cuda"),
+                      lse=torch.full((B, 2 * kv, T), 7.0, device="cuda"))
+    torch.cuda.synchronize()
+    there = np.broadcast_to((np.arange(T) < counts[:, None])[:, None], (B, 2 * kv, T))
+    check(out, lse, c.want(counts=counts), c.keys(), 64, False, there)
+    assert (out.float().cpu().numpy()[~there] == 7).all() and (lse.cpu().numpy()[~there] == 7).all()
+
+
 def test_lengths_past_the_table_are_clamped():
     c = Case(14, 2, 1, 1, 1, 64, 16, "int8", [32, 20])
     c.lengths = np.array([99999, -5])
