@@ -545,7 +545,7 @@ typedef struct sva_cache_query {
 } sva_cache_query;
 
 /* Bytes of device workspace that sva_cache_attention needs (partial results of
- * keys divided among workgroups, at most 66 MB; none for short page tables;
+ * keys divided among workgroups, at most 69 MB; none for short page tables;
  * the cache's pointers are not read).  Host only. */
 int sva_cache_attention_workspace(const sva_cache* cache, const sva_cache_query* query, size_t* bytes);
 
