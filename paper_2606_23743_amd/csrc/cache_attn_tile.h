@@ -45,6 +45,7 @@ void cache_tile_kernel(CacheAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char Vs[2][TB];
   __shared__ __attribute__((aligned(16))) float fs[2][kChunk], vs[2][kChunk];   // K scale * c * log2(e); V scale
   __shared__ __attribute__((aligned(16))) int lost[2][kWaves];   // whether a wave's rows of a stage have a key on a bad page
+  __shared__ uint64_t seen[2][RPT];                // which drafted keys of a stage each token of the tile sees
   __shared__ int not_finite;                       // some drafted value of the segment is Inf or NaN
 
   const int lane = threadIdx.x & 63, g = lane >> 4, i16 = lane & 15;
@@ -209,9 +210,33 @@ void cache_tile_kernel(CacheAttnArgs a) {
     const int d0 = max(u0 - en.cached_units, 0) * kUnit;
     const int d1 = a.kn.p ? min(en.cnt, (u1 - en.cached_units) * kUnit) : 0;
     const int nd = d1 > d0 ? (d1 - d0 + kChunk - 1) / kChunk : 0;
+    // tokens of the tile's rows; a wave looks at a token's 64 keys at once, eight tokens together
+    // (us against each lane's own keys one after the other: 4 sequences of 512 keys and 512 drafted
+    // tokens 110 / 86, 64 drafted ones 34 / 31, of one
+    // head in place of four 23 / 24; 8 of 8,192 and 60 level)
+    const int t0 = rt * RPT / a.G, t1 = min((rt * RPT + RPT - 1) / a.G, en.cnt - 1);
+    auto stage_seen = [&](int key0, int st) {
+      constexpr int UN = 8;
+      const int key = key0 + lane, wv = uniform((int)(threadIdx.x >> 6));
+#pragma unroll 1
+      for (int t = t0 + wv; t <= t1; t += 4 * UN) {
+        int is[UN];
+#pragma unroll
+        for (int k = 0; k < UN; ++k) {
+          const int tk = min(t + 4 * k, t1);
+          is[k] = a.mask ? (int)a.mask[b * a.mask_b + (int64_t)tk * a.T + min(key, a.T - 1)] : (int)(key <= tk);
+        }
+#pragma unroll
+        for (int k = 0; k < UN; ++k) {
+          const uint64_t bits = __builtin_amdgcn_ballot_w64(is[k] != 0 && key < d1);
+          if (lane == 0 && t + 4 * k <= t1) seen[st][t + 4 * k - t0] = bits;
+        }
+      }
+    };
     auto stage_drafts = [&](int key0, int st) {
       bool odd = false;
-#pragma unroll 1
+      stage_seen(key0, st);
+#pragma unroll 2
       for (int y = threadIdx.x; y < kChunk * G::NCH; y += 256) {
         const int row = y / G::NCH, c = y % G::NCH, key = key0 + row;
         u32x4 kk{}, vv{};
@@ -248,18 +273,11 @@ void cache_tile_kernel(CacheAttnArgs a) {
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) on[qt] = bits;
     };
-    auto seen_drafts = [&](int key0, int (&on)[QT]) {
+    auto seen_drafts = [&](int st, int sub, int (&on)[QT]) {
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        const int t = max(tok[qt], 0);
-        const uint8_t* mk = a.mask ? a.mask + b * a.mask_b + (int64_t)t * a.T : nullptr;
-        on[qt] = 0;
-#pragma unroll 1
-        for (int e = 0; e < 8; ++e) {
-          const int key = key0 + key_of(e);
-          const bool is = tok[qt] >= 0 && key < d1 && (mk ? mk[min(key, a.T - 1)] != 0 : key <= t);
-          on[qt] |= is ? 1 << e : 0;
-        }
+        const uint32_t x = tok[qt] >= 0 ? (uint32_t)(seen[st][tok[qt] - t0] >> (32 * sub)) : 0u;
+        on[qt] = (int)((x >> 4 * g & 15u) | (x >> (16 + 4 * g) & 15u) << 4);
       }
     };
 
@@ -438,7 +456,7 @@ void cache_tile_kernel(CacheAttnArgs a) {
 #pragma unroll
           for (int y = 0; y < NS; ++y) {
             if (cached) seen_cached(key0 + 32 * (sub + y), on[y]);
-            else seen_drafts(key0 + 32 * (sub + y), on[y]);
+            else seen_drafts(st, sub + y, on[y]);
           }
         }
         step(st, sub, whole, on);
@@ -460,6 +478,7 @@ void cache_tile_kernel(CacheAttnArgs a) {
 #pragma unroll 1
       for (int at = 0; at < 3 * nd; ++at) {
         const int kind = at % 3, key0 = d0 + at / 3 * kChunk;
+        stage_seen(key0, 0);
 #pragma unroll 1
         for (int y = threadIdx.x; y < kChunk * D; y += 256) {
           const int row = y / D, d = y % D, key = key0 + row;
@@ -473,7 +492,7 @@ void cache_tile_kernel(CacheAttnArgs a) {
 #pragma unroll 1
         for (int sub = 0; sub < 2; ++sub) {
           int on[QT];
-          seen_drafts(key0 + 32 * sub, on);
+          seen_drafts(0, sub, on);
           float one[QT][8];
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt)
