@@ -11,7 +11,8 @@ qknorm_rope.py with its own readings; feat_norm token pruning (Section 4.2.3;
 Appendix A.2.2 keeps 50% of video tokens by that score) in token_prune.py;
 8-bit attention (Section 4.2.4 points to the SageAttention series) in
 fp8_attention.py; the first-order remainder of non-kept blocks (Section 4.2.2)
-in remainder.py.
+in remainder.py.  1-D rotary positions are in rotary.py, the quantised key/value cache
+and the attention of drafted tokens over it in kv_cache.py (neither is the paper's).
 
 What the paper fixes (Section 4.2.2, "Sparse Attention"; Appendix A.2.2, the
 LTX-2.3 pipeline): attention over the spatiotemporal token set is replaced by a
