@@ -3,8 +3,9 @@
 //
 // What bounds it: from about 64 rows on a code that is read once meets enough rows
 // that widening it, the softmax and the products take longer than reading it (8 ragged
-// sequences of up to 75,600 int8 tokens, 6 heads of 128, up to 192 rows: 186 MB and 69 GFLOP in
-// 105 us, 660 TFLOP/s), and
+// sequences of up to 75,600 int8 tokens, 6 heads of 128, up to 192 rows: 353 MB and 65 GFLOP in
+// 175 us; at full tiles, 8 x 32,768 keys and 128 rows, 103 GFLOP in 155 us, 670 TFLOP/s: vector instructions issue
+// in 60% of the cycles, matrix cores are busy in 32%), and
 // if every wave widened its own keys, widening would come before the products.  So
 // the workgroup's four waves own QT tiles of 16 rows each and share the keys: 64 at
 // a time are widened once, by all lanes together, into row-major bf16 tiles in LDS
@@ -25,7 +26,10 @@ namespace cattn {
 
 constexpr int kChunk = 64;       // keys of a stage
 
-template <int FMT, int D, int QT, int NP, int AHEAD>
+// ONE: pages hold whole stages, so that a stage's page and the address of its first row are scalars
+// (per row they were a sixth of the vector instructions: 8 ragged sequences of up to 75,600 int8 tokens, up to
+// 192 rows, 197 us in pages of 64 without, 187 with)
+template <int FMT, int D, int QT, int NP, int AHEAD, bool ONE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void cache_tile_kernel(CacheAttnArgs a) {
   using G = attn::Geo<D>;
@@ -137,6 +141,10 @@ void cache_tile_kernel(CacheAttnArgs a) {
     const float* scales = threadIdx.x < kChunk ? a.c.ks : a.c.vs;
     auto load_pages = [&](int c) {
       const int key0 = k0 + c * kChunk;
+      if constexpr (ONE) {
+        spg = page_at(key0);
+        return;
+      }
 #pragma unroll
       for (int r = 0; r < NR; ++r) pg[r] = page_at(key0 + srow + r * RPP);
       if constexpr (W8) spg = page_at(key0 + (threadIdx.x & (kChunk - 1)));
@@ -149,6 +157,31 @@ void cache_tile_kernel(CacheAttnArgs a) {
       int64_t at[NR], sat = 0;
       bool sin = false;
       x.lost = false;
+      if constexpr (ONE) {                         // the chunk's page, and its first row: scalars
+        const int page = uniform(spg);
+        const bool there = page >= 0 && page < a.c.num_pages;
+        const int64_t row0 = there ? (((int64_t)page * Hkv + h) << log2p) + (key0 & pmask) : 0;
+        x.lost = !there;
+        if constexpr (W8) {
+          sin = there && key0 + (int)(threadIdx.x & (kChunk - 1)) < k1;
+          sat = row0 + (threadIdx.x & (kChunk - 1));
+        }
+        load_pages(c + 1);
+        const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + row0 * (D * EB);
+        const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + row0 * (D * EB);
+        const int off = srow * (D * EB) + min(piece, PIECES - 1) * 16;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          x.keep[r] = there && key0 + srow + r * RPP < k1 && piece < PIECES;
+          x.k[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + off + r * RPP * D * EB));
+          x.v[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + off + r * RPP * D * EB));
+        }
+        if constexpr (W8) {
+          x.scale = scales[sat];
+          x.scaled = sin;
+        }
+        return;
+      }
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         const int key = key0 + srow + r * RPP;
@@ -558,8 +591,12 @@ void cache_tile_kernel(CacheAttnArgs a) {
 template <int FMT, int D, int QT>
 void launch_tile(const CacheAttnArgs& a, int wgs, hipStream_t stream) {
   constexpr int kAhead = QT == 1 ? 2 : 1;
-  if (a.out_f32) hipLaunchKernelGGL((cache_tile_kernel<FMT, D, QT, 3, kAhead>), dim3(wgs), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((cache_tile_kernel<FMT, D, QT, 1, kAhead>), dim3(wgs), dim3(256), 0, stream, a);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(wgs), dim3(256), 0, stream, a); };
+  const bool one = 1 << a.c.log2_page >= kChunk;
+  if (a.out_f32 && one) go(cache_tile_kernel<FMT, D, QT, 3, kAhead, true>);
+  else if (a.out_f32) go(cache_tile_kernel<FMT, D, QT, 3, kAhead, false>);
+  else if (one) go(cache_tile_kernel<FMT, D, QT, 1, kAhead, true>);
+  else go(cache_tile_kernel<FMT, D, QT, 1, kAhead, false>);
 }
 
 }  // namespace cattn

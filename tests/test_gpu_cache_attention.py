@@ -85,6 +85,16 @@ def test_row_tiles_and_trees(G, T, fmt, D):
     c.run(mask=trees(c.g, 2, T))
 
 
+@pytest.mark.parametrize("page", [16, 64, 128, 256])
+@pytest.mark.parametrize("fmt,D,G,T", [("bf16", 128, 4, 20), ("e4m3", 112, 2, 100), ("int8", 64, 3, 40), ("int8", 128, 1, 130)])
+def test_many_rows_lengths_around_tiles_and_bad_pages(page, fmt, D, G, T):
+    n = [0, 1, 63, 64, 65, 129, 700, 1000]
+    c = Case(page + T, len(n), 1, G, T, D, page, fmt, n)
+    c.table[5, 0] = -1
+    c.table[6, -1 if page > 64 else 3] = c.values["k"].shape[0] + 5
+    c.run(mask=trees(c.g, len(n), T))
+
+
 @pytest.mark.parametrize("fmt,D,T", itertools.product(["bf16", "e4m3", "int8"], [64, 112, 128], [9, 40]))
 def test_float32_result(fmt, D, T):
     c = Case(T, 2, 1, 2, T, D, 64, fmt, [200, 77])
