@@ -85,6 +85,15 @@ def test_row_tiles_and_trees(G, T, fmt, D):
     c.run(mask=trees(c.g, 2, T))
 
 
+@pytest.mark.parametrize("G,T", [(16, 2), (33, 1), (12, 4), (7, 7), (49, 1), (64, 1), (64, 2), (129, 1), (64, 4), (257, 1), (1, 257)])
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+def test_rows_on_both_sides_of_each_form(G, T, fmt):
+    c = Case(G + T, 2, 1, G, T, 64, 64, fmt, [1100, 70])
+    counts = np.array([T, max(1, T - 1)])
+    rows = np.broadcast_to(np.arange(T)[None, None] < counts[:, None, None], (2, G, T))
+    c.run(mask=trees(c.g, 2, T), counts=counts, rows=rows)
+
+
 @pytest.mark.parametrize("page", [16, 64, 128, 256])
 @pytest.mark.parametrize("fmt,D,G,T", [("bf16", 128, 4, 20), ("e4m3", 112, 2, 100), ("int8", 64, 3, 40), ("int8", 128, 1, 130)])
 def test_many_rows_lengths_around_tiles_and_bad_pages(page, fmt, D, G, T):
