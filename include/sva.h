@@ -473,9 +473,9 @@ typedef struct sva_rotary_params {
  * Outputs must not share memory with each other or with the other tensor's
  * input (slices of one buffer may interleave).  The angle is formed and
  * reduced modulo one turn in float64, cosine, sine and the products in
- * float32, each result rounded once.  Data aligned to their elements; tensors
- * whose data and strides are multiples of 16 bytes (rot_dim of 8 elements in
- * bf16 or 4 in float32, twice that in the half layout) take 16-byte accesses. */
+ * float32, each result rounded once.  Data aligned to their elements; accesses
+ * are the largest of 16, 8, 4 and 2 bytes that data and strides, head_dim and
+ * rot_dim (half layout: half of it) are multiples of. */
 int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* positions,
                int64_t pos_stride_b, const sva_heads* q_in, const sva_heads* q_out,
                const sva_heads* k_in, const sva_heads* k_out, void* stream);

@@ -21,7 +21,8 @@ struct RotaryArgs {
   int64_t pos_b;
   int B, N, D, rot;
   float magnitude;
-  bool f32, half, backward, vec; // vec: every access can be 16 bytes
+  bool f32, half, backward;
+  int piece;                     // bytes of an access: 16, 8, 4 or (bf16) 2
   bool copy;                     // channels from rot on have to be copied
 };
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);

@@ -12,6 +12,8 @@
 // of a million are as exact as small ones), then streams rows, 16 bytes an
 // access, a lane's three to six items in flight together.  63,240 tokens of 40 heads of 128, half
 // of each turned: 222 us, 5.8 TB/s; 2 x 7,801 float32 tokens of 40 heads of 112: 97 us, 5.8 TB/s.
+#include <type_traits>
+
 #include "sva_internal.h"
 
 namespace sva {
@@ -21,6 +23,7 @@ constexpr int kThreads = 256;
 constexpr int kTab = 2048;       // (cos, sin) entries of a workgroup
 constexpr int kMaxTok = 16;      // tokens of a workgroup
 
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
@@ -31,63 +34,64 @@ struct RotaryGrid {
   int rot_items, row_items;      // items of a row that turn, and all of them
 };
 
-template <bool NT>
-__device__ __forceinline__ u32x4 load16(const void* p) {
-  if constexpr (NT) return __builtin_nontemporal_load(static_cast<const u32x4*>(p));
-  return *static_cast<const u32x4*>(p);
+// VB bytes (16, 8, 4 or 2: what sizes and strides are multiples of) at p as dwords.  30,703 bf16 tokens of
+// 8 heads of 112 with 56 turned in halves: 80 us by elements, 25 by 8 bytes; 8 x 8,403 of 18 with 54 in
+// pairs 341 and 274 by 4
+template <int VB, bool NT>
+__device__ __forceinline__ void load_piece(const void* p, uint32_t (&w)[(VB + 3) / 4]) {
+  using W = std::conditional_t<VB == 16, u32x4, std::conditional_t<VB == 8, u32x2, std::conditional_t<VB == 4, uint32_t, uint16_t>>>;
+  W x;
+  if constexpr (NT) x = __builtin_nontemporal_load(static_cast<const W*>(p));
+  else x = *static_cast<const W*>(p);
+  if constexpr (VB <= 4) {
+    w[0] = x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VB / 4; ++i) w[i] = x[i];
+  }
 }
-template <bool NT>
-__device__ __forceinline__ void store16(void* p, u32x4 v) {
-  if constexpr (NT) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
-  else *static_cast<u32x4*>(p) = v;
+template <int VB, bool NT>
+__device__ __forceinline__ void store_piece(void* p, const uint32_t (&w)[(VB + 3) / 4]) {
+  using W = std::conditional_t<VB == 16, u32x4, std::conditional_t<VB == 8, u32x2, std::conditional_t<VB == 4, uint32_t, uint16_t>>>;
+  W x;
+  if constexpr (VB <= 4) {
+    x = (W)w[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < VB / 4; ++i) x[i] = w[i];
+  }
+  if constexpr (NT) __builtin_nontemporal_store(x, static_cast<W*>(p));
+  else *static_cast<W*>(p) = x;
 }
 
-template <bool F32> struct Elem;
-template <> struct Elem<false> {
-  typedef uint16_t T;
-  static __device__ __forceinline__ float get(T x) { return __uint_as_float((uint32_t)x << 16); }
-  static __device__ __forceinline__ T put(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-  // 16 bytes as 8 floats and back
-  static constexpr int E = 8;
-  static __device__ __forceinline__ void wide(const u32x4& w, float (&y)[E]) {
+// a piece's E elements as floats, and back (bf16: to nearest, ties to even)
+template <bool F32, int E, int N>
+__device__ __forceinline__ void wide(const uint32_t (&w)[N], float (&y)[E]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[2 * i] = __uint_as_float(w[i] << 16);
-      y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  for (int e = 0; e < E; ++e) {
+    if constexpr (F32) y[e] = __uint_as_float(w[e]);
+    else y[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+  }
+}
+template <bool F32, int E, int N>
+__device__ __forceinline__ void narrow(const float (&y)[E], uint32_t (&w)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (F32) {
+      w[i] = __float_as_uint(y[i]);
+    } else {
+      const f32x2 f = {y[2 * i], E > 1 ? y[E > 1 ? 2 * i + 1 : 0] : 0.0f};
+      w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
     }
   }
-  static __device__ __forceinline__ u32x4 narrow(const float (&y)[E]) {
-    u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x2 f = {y[2 * i], y[2 * i + 1]};
-      w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));   // nearest, ties to even
-    }
-    return w;
-  }
-};
-template <> struct Elem<true> {
-  typedef float T;
-  static __device__ __forceinline__ float get(T x) { return x; }
-  static __device__ __forceinline__ T put(float x) { return x; }
-  static constexpr int E = 4;
-  static __device__ __forceinline__ void wide(const u32x4& w, float (&y)[E]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(w[i]);
-  }
-  static __device__ __forceinline__ u32x4 narrow(const float (&y)[E]) {
-    u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(y[i]);
-    return w;
-  }
-};
+}
 
-template <bool F32, bool HALF, bool VEC, int kUnroll, bool NT, bool BY_HEAD>
+template <bool F32, bool HALF, int VB, int kUnroll, bool NT, bool BY_HEAD>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGrid gr) {
-  using El = Elem<F32>;
-  using T = typename El::T;
-  constexpr int E = VEC ? El::E : 1;
+  using T = std::conditional_t<F32, float, uint16_t>;
+  constexpr int E = VB / (int)sizeof(T);       // elements of a piece
+  constexpr bool TWO = HALF || E == 1;         // a pair lies in two pieces
+  constexpr int NW = (VB + 3) / 4;
   __shared__ float2 tab[kTab];
   __shared__ int64_t base[kMaxTok][4];         // offsets of a token in q_in, q_out, k_in, k_out
 
@@ -138,85 +142,71 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
       cs[u] = tab + tk * np;
     }
     auto live = [&](int u) { return i0 + u * kThreads + (int)threadIdx.x < items; };
-    if constexpr (VEC) {
-      u32x4 w[kUnroll][2];
-      int at[kUnroll][2];                      // first channels of an item's one or two pieces
+    uint32_t w[kUnroll][2][NW];
+    int at[kUnroll][2];                        // first channels of an item's one or two pieces
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const bool turns = c[u] < gr.rot_items;
-        at[u][0] = turns ? c[u] * E : a.rot + (c[u] - gr.rot_items) * E;
-        at[u][1] = HALF && turns ? at[u][0] + np : at[u][0];
-        w[u][0] = load16<NT>(src[u] + at[u][0]);
-        if constexpr (HALF) w[u][1] = load16<NT>(src[u] + at[u][1]);
-      }
+    for (int u = 0; u < kUnroll; ++u) {
+      const bool turns = c[u] < gr.rot_items;
+      at[u][0] = turns ? c[u] * (TWO && !HALF ? 2 : E) : a.rot + (c[u] - gr.rot_items) * E;
+      at[u][1] = TWO && turns ? at[u][0] + (HALF ? np : 1) : at[u][0];
+      load_piece<VB, NT>(src[u] + at[u][0], w[u][0]);
+      if constexpr (TWO) load_piece<VB, NT>(src[u] + at[u][1], w[u][1]);
+    }
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        if (!live(u)) continue;
-        if (c[u] < gr.rot_items) {
-          float y[E], z[E];
-          El::wide(w[u][0], y);
-          if constexpr (HALF) {
-            El::wide(w[u][1], z);
+    for (int u = 0; u < kUnroll; ++u) {
+      if (!live(u)) continue;
+      if (c[u] < gr.rot_items) {
+        float y[E];
+        wide<F32, E>(w[u][0], y);
+        if constexpr (TWO) {
+          float z[E];
+          wide<F32, E>(w[u][1], z);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float2 t = cs[u][c[u] * E + e];
-              const float p = y[e], q = z[e];
-              y[e] = p * t.x - q * t.y;
-              z[e] = p * t.y + q * t.x;
-            }
-            store16<NT>(dst[u] + at[u][1], El::narrow(z));
-          } else {
-#pragma unroll
-            for (int e = 0; e < E / 2; ++e) {
-              const float2 t = cs[u][c[u] * (E / 2) + e];
-              const float p = y[2 * e], q = y[2 * e + 1];
-              y[2 * e] = p * t.x - q * t.y;
-              y[2 * e + 1] = p * t.y + q * t.x;
-            }
+          for (int e = 0; e < E; ++e) {
+            const float2 t = cs[u][c[u] * E + e];
+            const float p = y[e], q = z[e];
+            y[e] = p * t.x - q * t.y;
+            z[e] = p * t.y + q * t.x;
           }
-          w[u][0] = El::narrow(y);
-        } else if (src[u] == dst[u]) {
-          continue;                            // in place: nothing to copy
-        }
-        store16<NT>(dst[u] + at[u][0], w[u][0]);
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        if (!live(u)) continue;
-        if (c[u] < gr.rot_items) {             // one pair
-          const int i = HALF ? c[u] : 2 * c[u], j = HALF ? c[u] + np : 2 * c[u] + 1;
-          const float2 t = cs[u][c[u]];
-          const float p = El::get(src[u][i]), q = El::get(src[u][j]);
-          dst[u][i] = El::put(p * t.x - q * t.y);
-          dst[u][j] = El::put(p * t.y + q * t.x);
+          narrow<F32, E>(z, w[u][1]);
+          store_piece<VB, NT>(dst[u] + at[u][1], w[u][1]);
         } else {
-          const int i = a.rot + c[u] - gr.rot_items;
-          dst[u][i] = src[u][i];
+#pragma unroll
+          for (int e = 0; e < E / 2; ++e) {
+            const float2 t = cs[u][c[u] * (E / 2) + e];
+            const float p = y[2 * e], q = y[2 * e + 1];
+            y[2 * e] = p * t.x - q * t.y;
+            y[2 * e + 1] = p * t.y + q * t.x;
+          }
         }
+        narrow<F32, E>(y, w[u][0]);
+      } else if (src[u] == dst[u]) {
+        continue;                              // in place: nothing to copy
       }
+      store_piece<VB, NT>(dst[u] + at[u][0], w[u][0]);
     }
   }
 }
 
-template <bool F32, bool HALF, bool VEC, int U>
+template <bool F32, bool HALF, int VB, int U>
 void launch_unroll(const RotaryArgs& a, const RotaryGrid& gr, bool nt, hipStream_t stream) {
   const int64_t tokens = (int64_t)a.B * a.N;
   const int heads = a.qi.heads + a.ki.heads;
   const dim3 grid((unsigned)((tokens + gr.tok - 1) / gr.tok), (heads + gr.heads - 1) / gr.heads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a, gr); };
-  if (gr.by_head && nt) go(rotary_kernel<F32, HALF, VEC, U, VEC, true>);
-  else if (gr.by_head) go(rotary_kernel<F32, HALF, VEC, U, false, true>);
-  else if (nt) go(rotary_kernel<F32, HALF, VEC, U, VEC, false>);
-  else go(rotary_kernel<F32, HALF, VEC, U, false, false>);
+  if (gr.by_head && nt) go(rotary_kernel<F32, HALF, VB, U, VB == 16, true>);
+  else if (gr.by_head) go(rotary_kernel<F32, HALF, VB, U, false, true>);
+  else if (nt) go(rotary_kernel<F32, HALF, VB, U, VB == 16, false>);
+  else go(rotary_kernel<F32, HALF, VB, U, false, false>);
 }
 
-template <bool F32, bool HALF, bool VEC>
+template <bool F32, bool HALF, int VB>
 void launch_as(const RotaryArgs& a, hipStream_t stream) {
-  constexpr int E = VEC ? Elem<F32>::E : 1, kItem = F32 ? 4 : 2;
+  constexpr int kItem = F32 ? 4 : 2, E = VB / kItem;
+  constexpr bool TWO = HALF || E == 1;
   const int heads = a.qi.heads + a.ki.heads;
   RotaryGrid gr{1, heads, false, 0, 0};
-  gr.rot_items = !VEC || HALF ? a.rot / 2 / E : a.rot / E;
+  gr.rot_items = TWO ? a.rot / 2 / E : a.rot / E;
   gr.row_items = gr.rot_items + (a.copy ? (a.D - a.rot) / E : 0);
   // Where a head's tokens lie together (not a token's heads), a workgroup takes 4 KB of each of
   // as many heads as make four items a lane; us against all heads of fewer tokens, 2 x 7,801
@@ -237,7 +227,7 @@ void launch_as(const RotaryArgs& a, hipStream_t stream) {
   // slower: 63,240 tokens of 40 heads of 128, half turned, 220 us in one, 262 in four.
   int unroll = 4;
   double best = 0.0;
-  for (int u = 3; u <= 6; ++u) {
+  for (int u = VB < 16 ? 6 : 3; u <= 6; ++u) {
     int64_t t = (int64_t)u * kThreads / per_token;
     t = t < kMaxTok ? t : kMaxTok;
     t = t < kTab / (a.rot / 2) ? t : kTab / (a.rot / 2);
@@ -257,17 +247,19 @@ void launch_as(const RotaryArgs& a, hipStream_t stream) {
   const bool lines = !HALF || a.rot / 2 * kItem % 128 == 0;
   const int64_t bytes = (int64_t)a.B * a.N * (a.qi.heads + a.ki.heads) * a.D * kItem;
   const bool nt = lines && bytes >= (64 << 20);
-  if constexpr (!VEC) launch_unroll<F32, HALF, VEC, 4>(a, gr, false, stream);
-  else if (unroll == 3) launch_unroll<F32, HALF, VEC, 3>(a, gr, nt, stream);
-  else if (unroll == 4) launch_unroll<F32, HALF, VEC, 4>(a, gr, nt, stream);
-  else if (unroll == 5) launch_unroll<F32, HALF, VEC, 5>(a, gr, nt, stream);
-  else launch_unroll<F32, HALF, VEC, 6>(a, gr, nt, stream);
+  if constexpr (VB < 16) launch_unroll<F32, HALF, VB, 6>(a, gr, false, stream);
+  else if (unroll == 3) launch_unroll<F32, HALF, VB, 3>(a, gr, nt, stream);
+  else if (unroll == 4) launch_unroll<F32, HALF, VB, 4>(a, gr, nt, stream);
+  else if (unroll == 5) launch_unroll<F32, HALF, VB, 5>(a, gr, nt, stream);
+  else launch_unroll<F32, HALF, VB, 6>(a, gr, nt, stream);
 }
 
 template <bool F32, bool HALF>
 void launch_layout(const RotaryArgs& a, hipStream_t stream) {
-  if (a.vec) launch_as<F32, HALF, true>(a, stream);
-  else launch_as<F32, HALF, false>(a, stream);
+  if (a.piece == 16) launch_as<F32, HALF, 16>(a, stream);
+  else if (a.piece == 8) launch_as<F32, HALF, 8>(a, stream);
+  else if (F32 || a.piece == 4) launch_as<F32, HALF, 4>(a, stream);
+  else if constexpr (!F32) launch_as<F32, HALF, 2>(a, stream);
 }
 
 }  // namespace

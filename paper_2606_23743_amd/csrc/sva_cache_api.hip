@@ -23,7 +23,7 @@ int hip_status(hipError_t e) { return e == hipSuccess ? SVA_OK : SVA_ERR_HIP; }
 struct Tensor {
   HeadsView v;
   size_t span;
-  bool vec;                      // data and strides are multiples of 16 bytes
+  int align;                     // what data and strides are multiples of: 16, 8, 4 or 2 bytes
 };
 
 int check_heads(const sva_heads* h, int64_t B, int64_t N, int64_t D, size_t item, bool wide, bool output, Tensor* t) {
@@ -40,9 +40,14 @@ int check_heads(const sva_heads* h, int64_t B, int64_t N, int64_t D, size_t item
     if (__builtin_mul_overflow(d.size - 1, d.stride, &x) || __builtin_add_overflow(span, x, &span)) return SVA_ERR_SHAPE;
   }
   if (span > ((int64_t)1 << 58)) return SVA_ERR_SHAPE;
-  bool vec = aligned(h->data, 16);
-  for (const Dim& d : dims) vec = vec && d.stride * (int64_t)item % 16 == 0;
-  if (!aligned(h->data, item) || (wide && !vec)) return SVA_ERR_ALIGNMENT;
+  int align = 16;
+  auto fits = [&](int n) {
+    bool all = aligned(h->data, n);
+    for (const Dim& d : dims) all = all && d.stride * (int64_t)item % n == 0;
+    return all;
+  };
+  while (align > (int)item && !fits(align)) align /= 2;
+  if (!aligned(h->data, item) || (wide && align < 16)) return SVA_ERR_ALIGNMENT;
   if (output) {                  // rows must not overlap
     std::sort(dims, dims + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
     int64_t reach = D;
@@ -58,7 +63,7 @@ int check_heads(const sva_heads* h, int64_t B, int64_t N, int64_t D, size_t item
   t->v.sn = h->stride_n;
   t->v.heads = h->heads;
   t->span = (size_t)span * item;
-  t->vec = vec;
+  t->align = align;
   return SVA_OK;
 }
 
@@ -208,7 +213,8 @@ int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* po
   if (qi.v.heads != qo.v.heads) return SVA_ERR_SHAPE;
   const bool q_place = same(qi, qo, B, N);
   if (!q_place && !apart(qi, qo)) return SVA_ERR_INVALID_ARG;
-  bool vec = qi.vec && qo.vec, k_place = true;
+  int piece = std::min(qi.align, qo.align);
+  bool k_place = true;
   if (k_in) {
     if ((st = check_heads(k_in, B, N, D, item, false, false, &ki)) != SVA_OK) return st;
     if ((st = check_heads(k_out, B, N, D, item, false, true, &ko)) != SVA_OK) return st;
@@ -216,10 +222,9 @@ int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* po
     k_place = same(ki, ko, B, N);
     if (!k_place && !apart(ki, ko)) return SVA_ERR_INVALID_ARG;
     if (qo.v.p == ko.v.p || qo.v.p == ki.v.p || ko.v.p == qi.v.p) return SVA_ERR_INVALID_ARG;
-    vec = vec && ki.vec && ko.vec;
+    piece = std::min({piece, ki.align, ko.align});
   }
   if ((int64_t)qi.v.heads + ki.v.heads > 1 << 20) return SVA_ERR_SHAPE;
-  const int e = (int)(16 / item);
   sva::RotaryArgs a{};
   a.qi = qi.v;
   a.qo = qo.v;
@@ -237,7 +242,10 @@ int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* po
   a.half = p->layout == SVA_ROTARY_HALF;
   a.backward = p->backward != 0;
   a.copy = !(q_place && k_place);
-  a.vec = vec && p->rot_dim % (a.half ? 2 * e : e) == 0 && (!a.copy || p->head_dim % e == 0);
+  // bytes of an access: a whole number of them makes the turned part (each half of it) and the rest
+  const int64_t turned = (int64_t)p->rot_dim * item / (a.half ? 2 : 1), row = a.copy ? D * (int64_t)item : 0;
+  while (piece > (int)item && (turned % piece != 0 || row % piece != 0)) piece /= 2;
+  a.piece = piece;
   return hip_status(sva::launch_rotary(a, static_cast<hipStream_t>(stream)));
 }
 
