@@ -474,8 +474,9 @@ typedef struct sva_rotary_params {
  * input (slices of one buffer may interleave).  The angle is formed and
  * reduced modulo one turn in float64, cosine, sine and the products in
  * float32, each result rounded once.  Data aligned to their elements; accesses
- * are the largest of 16, 8, 4 and 2 bytes that data and strides, head_dim and
- * rot_dim (half layout: half of it) are multiples of. */
+ * are of 16 bytes where data, strides and the channels turned (half layout:
+ * half of them) and kept are multiples of 4 bytes and 16 or more of them (or
+ * none); else of 8, 4 or 2. */
 int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* positions,
                int64_t pos_stride_b, const sva_heads* q_in, const sva_heads* q_out,
                const sva_heads* k_in, const sva_heads* k_out, void* stream);

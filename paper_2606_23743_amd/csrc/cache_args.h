@@ -23,6 +23,7 @@ struct RotaryArgs {
   float magnitude;
   bool f32, half, backward;
   int piece;                     // bytes of an access: 16, 8, 4 or (bf16) 2
+  bool ragged;                   // piece 8 or 4: the turned part (each half) and the rest hold 16 bytes or are none
   bool copy;                     // channels from rot on have to be copied
 };
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);

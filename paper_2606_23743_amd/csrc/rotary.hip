@@ -25,6 +25,7 @@ constexpr int kMaxTok = 16;      // tokens of a workgroup
 
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef u32x4 __attribute__((aligned(4))) u32x4a;   // at any dword
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
@@ -34,14 +35,17 @@ struct RotaryGrid {
   int rot_items, row_items;      // items of a row that turn, and all of them
 };
 
-// VB bytes (16, 8, 4 or 2: what sizes and strides are multiples of) at p as dwords.  30,703 bf16 tokens of
-// 8 heads of 112 with 56 turned in halves: 80 us by elements, 25 by 8 bytes; 8 x 8,403 of 18 with 54 in
-// pairs 341 and 274 by 4
-template <int VB, bool NT>
+// VB bytes at p as dwords: 16, or the largest of 8, 4 and 2 that sizes and strides are multiples of.
+// RAGGED: 16 bytes at any dword, where regions are multiples of four bytes and hold 16: a region's last
+// piece begins so much earlier that it ends with the region, and stores what is its own.  us, by
+// elements / by 8 or 4 bytes / RAGGED, bf16: 30,703 tokens of 8 heads of 112, 56 turned in halves, 80 / 25 /
+// 26; 64 x 106 of 44, the same, 78 / 42 / 33; 8 x 8,403 of 18, 54 turned in pairs, 341 / 274 / 107
+template <int VB, bool NT, bool RAGGED>
 __device__ __forceinline__ void load_piece(const void* p, uint32_t (&w)[(VB + 3) / 4]) {
   using W = std::conditional_t<VB == 16, u32x4, std::conditional_t<VB == 8, u32x2, std::conditional_t<VB == 4, uint32_t, uint16_t>>>;
   W x;
-  if constexpr (NT) x = __builtin_nontemporal_load(static_cast<const W*>(p));
+  if constexpr (RAGGED) x = *static_cast<const u32x4a*>(p);
+  else if constexpr (NT) x = __builtin_nontemporal_load(static_cast<const W*>(p));
   else x = *static_cast<const W*>(p);
   if constexpr (VB <= 4) {
     w[0] = x;
@@ -50,7 +54,7 @@ __device__ __forceinline__ void load_piece(const void* p, uint32_t (&w)[(VB + 3)
     for (int i = 0; i < VB / 4; ++i) w[i] = x[i];
   }
 }
-template <int VB, bool NT>
+template <int VB, bool NT, bool RAGGED>
 __device__ __forceinline__ void store_piece(void* p, const uint32_t (&w)[(VB + 3) / 4]) {
   using W = std::conditional_t<VB == 16, u32x4, std::conditional_t<VB == 8, u32x2, std::conditional_t<VB == 4, uint32_t, uint16_t>>>;
   W x;
@@ -60,7 +64,8 @@ __device__ __forceinline__ void store_piece(void* p, const uint32_t (&w)[(VB + 3
 #pragma unroll
     for (int i = 0; i < VB / 4; ++i) x[i] = w[i];
   }
-  if constexpr (NT) __builtin_nontemporal_store(x, static_cast<W*>(p));
+  if constexpr (RAGGED) *static_cast<u32x4a*>(p) = x;
+  else if constexpr (NT) __builtin_nontemporal_store(x, static_cast<W*>(p));
   else *static_cast<W*>(p) = x;
 }
 
@@ -86,7 +91,7 @@ __device__ __forceinline__ void narrow(const float (&y)[E], uint32_t (&w)[N]) {
   }
 }
 
-template <bool F32, bool HALF, int VB, int kUnroll, bool NT, bool BY_HEAD>
+template <bool F32, bool HALF, int VB, bool RAGGED, int kUnroll, bool NT, bool BY_HEAD>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGrid gr) {
   using T = std::conditional_t<F32, float, uint16_t>;
   constexpr int E = VB / (int)sizeof(T);       // elements of a piece
@@ -142,6 +147,18 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
       cs[u] = tab + tk * np;
     }
     auto live = [&](int u) { return i0 + u * kThreads + (int)threadIdx.x < items; };
+    [[maybe_unused]] int skip[kUnroll];        // RAGGED: a piece's first elements that another item has
+    auto put = [&](T* to, const uint32_t (&x)[NW], int u) {
+      if constexpr (RAGGED) {
+        if (skip[u] > 0) {
+#pragma unroll
+          for (int i = 0; i < NW; ++i)
+            if (i * (E / NW) >= skip[u]) store_piece<4, false, false>(to + i * (E / NW), {x[i]});
+          return;
+        }
+      }
+      store_piece<VB, NT, RAGGED>(to, x);
+    };
     uint32_t w[kUnroll][2][NW];
     int at[kUnroll][2];                        // first channels of an item's one or two pieces
 #pragma unroll
@@ -149,8 +166,15 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
       const bool turns = c[u] < gr.rot_items;
       at[u][0] = turns ? c[u] * (TWO && !HALF ? 2 : E) : a.rot + (c[u] - gr.rot_items) * E;
       at[u][1] = TWO && turns ? at[u][0] + (HALF ? np : 1) : at[u][0];
-      load_piece<VB, NT>(src[u] + at[u][0], w[u][0]);
-      if constexpr (TWO) load_piece<VB, NT>(src[u] + at[u][1], w[u][1]);
+      if constexpr (RAGGED) {
+        // the region's last piece begins so much earlier that it ends with the region
+        const int end = turns ? (HALF ? np : a.rot) : a.D;
+        skip[u] = max(at[u][0] + E - end, 0);
+        at[u][0] -= skip[u];
+        at[u][1] -= skip[u];
+      }
+      load_piece<VB, NT, RAGGED>(src[u] + at[u][0], w[u][0]);
+      if constexpr (TWO) load_piece<VB, NT, RAGGED>(src[u] + at[u][1], w[u][1]);
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -163,17 +187,17 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
           wide<F32, E>(w[u][1], z);
 #pragma unroll
           for (int e = 0; e < E; ++e) {
-            const float2 t = cs[u][c[u] * E + e];
+            const float2 t = cs[u][(RAGGED ? at[u][0] : c[u] * E) + e];
             const float p = y[e], q = z[e];
             y[e] = p * t.x - q * t.y;
             z[e] = p * t.y + q * t.x;
           }
           narrow<F32, E>(z, w[u][1]);
-          store_piece<VB, NT>(dst[u] + at[u][1], w[u][1]);
+          put(dst[u] + at[u][1], w[u][1], u);
         } else {
 #pragma unroll
           for (int e = 0; e < E / 2; ++e) {
-            const float2 t = cs[u][c[u] * (E / 2) + e];
+            const float2 t = cs[u][(RAGGED ? at[u][0] / 2 : c[u] * (E / 2)) + e];
             const float p = y[2 * e], q = y[2 * e + 1];
             y[2 * e] = p * t.x - q * t.y;
             y[2 * e + 1] = p * t.y + q * t.x;
@@ -183,31 +207,32 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
       } else if (src[u] == dst[u]) {
         continue;                              // in place: nothing to copy
       }
-      store_piece<VB, NT>(dst[u] + at[u][0], w[u][0]);
+      put(dst[u] + at[u][0], w[u][0], u);
     }
   }
 }
 
-template <bool F32, bool HALF, int VB, int U>
+template <bool F32, bool HALF, int VB, bool RAGGED, int U>
 void launch_unroll(const RotaryArgs& a, const RotaryGrid& gr, bool nt, hipStream_t stream) {
   const int64_t tokens = (int64_t)a.B * a.N;
   const int heads = a.qi.heads + a.ki.heads;
   const dim3 grid((unsigned)((tokens + gr.tok - 1) / gr.tok), (heads + gr.heads - 1) / gr.heads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a, gr); };
-  if (gr.by_head && nt) go(rotary_kernel<F32, HALF, VB, U, VB == 16, true>);
-  else if (gr.by_head) go(rotary_kernel<F32, HALF, VB, U, false, true>);
-  else if (nt) go(rotary_kernel<F32, HALF, VB, U, VB == 16, false>);
-  else go(rotary_kernel<F32, HALF, VB, U, false, false>);
+  constexpr bool NT = VB == 16 && !RAGGED;
+  if (gr.by_head && nt) go(rotary_kernel<F32, HALF, VB, RAGGED, U, NT, true>);
+  else if (gr.by_head) go(rotary_kernel<F32, HALF, VB, RAGGED, U, false, true>);
+  else if (nt) go(rotary_kernel<F32, HALF, VB, RAGGED, U, NT, false>);
+  else go(rotary_kernel<F32, HALF, VB, RAGGED, U, false, false>);
 }
 
-template <bool F32, bool HALF, int VB>
+template <bool F32, bool HALF, int VB, bool RAGGED = false>
 void launch_as(const RotaryArgs& a, hipStream_t stream) {
   constexpr int kItem = F32 ? 4 : 2, E = VB / kItem;
   constexpr bool TWO = HALF || E == 1;
   const int heads = a.qi.heads + a.ki.heads;
   RotaryGrid gr{1, heads, false, 0, 0};
-  gr.rot_items = TWO ? a.rot / 2 / E : a.rot / E;
-  gr.row_items = gr.rot_items + (a.copy ? (a.D - a.rot) / E : 0);
+  gr.rot_items = ((TWO ? a.rot / 2 : a.rot) + E - 1) / E;
+  gr.row_items = gr.rot_items + (a.copy ? (a.D - a.rot + E - 1) / E : 0);
   // Where a head's tokens lie together (not a token's heads), a workgroup takes 4 KB of each of
   // as many heads as make four items a lane; us against all heads of fewer tokens, 2 x 7,801
   // tokens of 40 heads of 112: float32 115 / 97, bf16 interleaved 85 / 57, halves 61 / 52;
@@ -227,7 +252,8 @@ void launch_as(const RotaryArgs& a, hipStream_t stream) {
   // slower: 63,240 tokens of 40 heads of 128, half turned, 220 us in one, 262 in four.
   int unroll = 4;
   double best = 0.0;
-  for (int u = VB < 16 ? 6 : 3; u <= 6; ++u) {
+  constexpr int kOnly = RAGGED ? 4 : 6;
+  for (int u = VB < 16 || RAGGED ? kOnly : 3; u <= (RAGGED ? kOnly : 6); ++u) {
     int64_t t = (int64_t)u * kThreads / per_token;
     t = t < kMaxTok ? t : kMaxTok;
     t = t < kTab / (a.rot / 2) ? t : kTab / (a.rot / 2);
@@ -247,16 +273,17 @@ void launch_as(const RotaryArgs& a, hipStream_t stream) {
   const bool lines = !HALF || a.rot / 2 * kItem % 128 == 0;
   const int64_t bytes = (int64_t)a.B * a.N * (a.qi.heads + a.ki.heads) * a.D * kItem;
   const bool nt = lines && bytes >= (64 << 20);
-  if constexpr (VB < 16) launch_unroll<F32, HALF, VB, 6>(a, gr, false, stream);
-  else if (unroll == 3) launch_unroll<F32, HALF, VB, 3>(a, gr, nt, stream);
-  else if (unroll == 4) launch_unroll<F32, HALF, VB, 4>(a, gr, nt, stream);
-  else if (unroll == 5) launch_unroll<F32, HALF, VB, 5>(a, gr, nt, stream);
-  else launch_unroll<F32, HALF, VB, 6>(a, gr, nt, stream);
+  if constexpr (VB < 16 || RAGGED) launch_unroll<F32, HALF, VB, RAGGED, kOnly>(a, gr, false, stream);
+  else if (unroll == 3) launch_unroll<F32, HALF, VB, false, 3>(a, gr, nt, stream);
+  else if (unroll == 4) launch_unroll<F32, HALF, VB, false, 4>(a, gr, nt, stream);
+  else if (unroll == 5) launch_unroll<F32, HALF, VB, false, 5>(a, gr, nt, stream);
+  else launch_unroll<F32, HALF, VB, false, 6>(a, gr, nt, stream);
 }
 
 template <bool F32, bool HALF>
 void launch_layout(const RotaryArgs& a, hipStream_t stream) {
   if (a.piece == 16) launch_as<F32, HALF, 16>(a, stream);
+  else if (a.ragged) launch_as<F32, HALF, 16, true>(a, stream);
   else if (a.piece == 8) launch_as<F32, HALF, 8>(a, stream);
   else if (F32 || a.piece == 4) launch_as<F32, HALF, 4>(a, stream);
   else if constexpr (!F32) launch_as<F32, HALF, 2>(a, stream);

@@ -246,6 +246,8 @@ int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* po
   const int64_t turned = (int64_t)p->rot_dim * item / (a.half ? 2 : 1), row = a.copy ? D * (int64_t)item : 0;
   while (piece > (int)item && (turned % piece != 0 || row % piece != 0)) piece /= 2;
   a.piece = piece;
+  const int64_t rest = a.copy ? (D - p->rot_dim) * (int64_t)item : 0;
+  a.ragged = piece >= 4 && turned >= 16 && (rest == 0 || rest >= 16);
   return hip_status(sva::launch_rotary(a, static_cast<hipStream_t>(stream)));
 }
 

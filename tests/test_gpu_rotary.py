@@ -101,6 +101,13 @@ def test_heads_are_divided_where_a_heads_tokens_lie_together(B, H, Hk, N, D, rot
         _case(B, H, Hk, N, D, rot, layout, dtype, in_place=in_place)
 
 
+@pytest.mark.parametrize("layout,dtype,strides,in_place",
+                         itertools.product(["half", "interleaved"], ["bf16", "f32"], ["plain", "token", "odd"], [False, True]))
+@pytest.mark.parametrize("D,rot", [(112, 56), (64, 20), (128, 70), (128, 94), (64, 62), (66, 36), (40, 24), (24, 24)])
+def test_parts_that_are_no_multiple_of_an_access(D, rot, layout, dtype, strides, in_place):
+    _case(2, 5, 3, 41, D, rot, layout, dtype, strides=strides, in_place=in_place, backward=rot == 56)
+
+
 def test_more_heads_than_groups_may_be():
     _case(1, 66000, 1, 2, 64, 64, "half", "bf16")
 
