@@ -2,6 +2,10 @@
 every step of the path runs in the library's HIP kernels.  torch supplies device
 memory and the current stream; nothing here computes on the host, and there is
 no fallback -- a missing or unloadable library raises.
+
+A call with stream= (a torch stream or a handle) is launched there.  The caller
+puts that stream behind the work that makes the inputs, and the work that uses the
+outputs behind that stream; memory that the call allocates needs no such order.
 """
 from __future__ import annotations
 
@@ -250,12 +254,38 @@ def _side_stream(stream):
     return None if h == cur else torch.cuda.ExternalStream(h)
 
 
+def _output(stream, make, *args, **kw):
+    """make(*args, **kw), an output that a call on `stream` writes.  The caching
+    allocator hands out memory that was freed on a stream while kernels of that
+    stream may still use it, which is in order for that stream alone: so the memory
+    is taken on the call's stream, and marked for the current one, where the
+    caller uses (and frees) it."""
+    s = None if stream is None else _side_stream(stream)
+    if s is None:
+        return make(*args, **kw)
+    torch = _torch()
+    with torch.cuda.stream(s):
+        x = make(*args, **kw)
+    x.record_stream(torch.cuda.current_stream())
+    return x
+
+
+def _scratch(stream, nbytes, device):
+    """A workspace, which no other stream uses: taken on the call's stream."""
+    torch = _torch()
+    s = _side_stream(stream)
+    if s is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(s):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _record(stream, *tensors):
     """Mark every tensor a call reads or writes as in use on the call's stream
     when that is not the current stream: the caching allocator then keeps the
-    memory of a tensor freed meanwhile (a workspace or output allocated here
-    on the current stream, or an input the caller drops) from being handed to
-    another allocation until the work enqueued on that stream has finished."""
+    memory of a tensor freed meanwhile (an input or an output of the caller's,
+    who drops it) from being handed to another allocation until the work
+    enqueued on that stream has finished."""
     if stream is None:
         return
     s = _side_stream(stream)
@@ -296,11 +326,11 @@ def pool_blocks(prob: Problem, q, k, q_pool=None, k_pool=None, stream=None) -> T
     _need(k, torch.bfloat16, shp, "k")
     pshape = (prob.batch, prob.heads, nb, prob.head_dim)
     if q_pool is None:
-        q_pool = torch.empty(pshape, dtype=torch.float32, device=q.device)
+        q_pool = _output(stream, torch.empty, pshape, dtype=torch.float32, device=q.device)
     else:
         _need(q_pool, torch.float32, pshape, "q_pool")
     if k_pool is None:
-        k_pool = torch.empty(pshape, dtype=torch.float32, device=q.device)
+        k_pool = _output(stream, torch.empty, pshape, dtype=torch.float32, device=q.device)
     else:
         _need(k_pool, torch.float32, pshape, "k_pool")
     _check(load().sva_pool_blocks(ctypes.byref(prob), _ptr(q), _ptr(k), _ptr(q_pool), _ptr(k_pool),
@@ -322,20 +352,20 @@ def qknorm_rope_pool(prob: Problem, q_in, k_in, gamma_q, gamma_k, eps: float = 1
     _need(gamma_q, torch.float32, (prob.head_dim,), "gamma_q")
     _need(gamma_k, torch.float32, (prob.head_dim,), "gamma_k")
     if q_out is None:
-        q_out = torch.empty_like(q_in)
+        q_out = _output(stream, torch.empty_like, q_in)
     else:
         _need(q_out, torch.bfloat16, shp, "q_out")
     if k_out is None:
-        k_out = torch.empty_like(k_in)
+        k_out = _output(stream, torch.empty_like, k_in)
     else:
         _need(k_out, torch.bfloat16, shp, "k_out")
     pshape = (prob.batch, prob.heads, nb, prob.head_dim)
     if q_pool is None:
-        q_pool = torch.empty(pshape, dtype=torch.float32, device=q_in.device)
+        q_pool = _output(stream, torch.empty, pshape, dtype=torch.float32, device=q_in.device)
     else:
         _need(q_pool, torch.float32, pshape, "q_pool")
     if k_pool is None:
-        k_pool = torch.empty(pshape, dtype=torch.float32, device=q_in.device)
+        k_pool = _output(stream, torch.empty, pshape, dtype=torch.float32, device=q_in.device)
     else:
         _need(k_pool, torch.float32, pshape, "k_pool")
     rp = RopeParams(float(eps), float(rope_base))
@@ -358,15 +388,15 @@ def select_blocks(prob: Problem, sel: SelectParams, q_pool, k_pool, kmax: Option
         kmax = max_keep(prob, sel)
     dev = q_pool.device
     if kv_idx is None:
-        kv_idx = torch.empty((prob.batch, prob.heads, nb, kmax), dtype=torch.int32, device=dev)
+        kv_idx = _output(stream, torch.empty, (prob.batch, prob.heads, nb, kmax), dtype=torch.int32, device=dev)
     else:
         _need(kv_idx, torch.int32, (prob.batch, prob.heads, nb, kmax), "kv_idx")
     if kv_count is None:
-        kv_count = torch.empty((prob.batch, prob.heads, nb), dtype=torch.int32, device=dev)
+        kv_count = _output(stream, torch.empty, (prob.batch, prob.heads, nb), dtype=torch.int32, device=dev)
     else:
         _need(kv_count, torch.int32, (prob.batch, prob.heads, nb), "kv_count")
     if want_mask and mask is None:
-        mask = torch.empty((prob.batch, prob.heads, nb, nb), dtype=torch.uint8, device=dev)
+        mask = _output(stream, torch.empty, (prob.batch, prob.heads, nb, nb), dtype=torch.uint8, device=dev)
     if mask is not None:
         _need(mask, torch.uint8, (prob.batch, prob.heads, nb, nb), "mask")
     _check(load().sva_select_blocks(ctypes.byref(prob), ctypes.byref(sel), _ptr(q_pool), _ptr(k_pool),
@@ -376,11 +406,11 @@ def select_blocks(prob: Problem, sel: SelectParams, q_pool, k_pool, kmax: Option
     return kv_idx, kv_count, mask
 
 
-def _out_tensor(prob, like, out):
+def _out_tensor(prob, like, out, stream):
     torch = _torch()
     dt = torch.float32 if prob.out_dtype == SVA_F32 else torch.bfloat16
     if out is None:
-        return torch.empty(_qkv_shape(prob), dtype=dt, device=like.device)
+        return _output(stream, torch.empty, _qkv_shape(prob), dtype=dt, device=like.device)
     _need(out, dt, _qkv_shape(prob), "out")
     return out
 
@@ -395,9 +425,9 @@ def sparse_attention(prob: Problem, q, k, v, kv_idx, kv_count, out=None, want_ls
     kmax = kv_idx.shape[-1]
     _need(kv_idx, torch.int32, (prob.batch, prob.heads, nb, kmax), "kv_idx")
     _need(kv_count, torch.int32, (prob.batch, prob.heads, nb), "kv_count")
-    out = _out_tensor(prob, q, out)
+    out = _out_tensor(prob, q, out, stream)
     if want_lse and lse is None:
-        lse = torch.empty(shp[:3], dtype=torch.float32, device=q.device)
+        lse = _output(stream, torch.empty, shp[:3], dtype=torch.float32, device=q.device)
     if lse is not None:
         _need(lse, torch.float32, shp[:3], "lse")
     _check(load().sva_sparse_attention(ctypes.byref(prob), _ptr(q), _ptr(k), _ptr(v), _ptr(kv_idx),
@@ -430,11 +460,11 @@ def block_moments(prob: Problem, k, v, kbar=None, vbar=None, moments=None, strea
     for t, n in ((k, "k"), (v, "v")):
         _need(t, torch.bfloat16, shp, n)
     if kbar is None:
-        kbar = torch.empty((B, H, nb, D), dtype=torch.bfloat16, device=k.device)
+        kbar = _output(stream, torch.empty, (B, H, nb, D), dtype=torch.bfloat16, device=k.device)
     if vbar is None:
-        vbar = torch.empty((B, H, nb, D), dtype=torch.bfloat16, device=k.device)
+        vbar = _output(stream, torch.empty, (B, H, nb, D), dtype=torch.bfloat16, device=k.device)
     if moments is None:
-        moments = torch.empty((B, H, nb, D, D), dtype=torch.bfloat16, device=k.device)
+        moments = _output(stream, torch.empty, (B, H, nb, D, D), dtype=torch.bfloat16, device=k.device)
     _need(kbar, torch.bfloat16, (B, H, nb, D), "kbar")
     _need(vbar, torch.bfloat16, (B, H, nb, D), "vbar")
     _need(moments, torch.bfloat16, (B, H, nb, D, D), "moments")
@@ -461,13 +491,13 @@ def sparse_attention_remainder(prob: Problem, q, k, v, q_pool, k_pool, kv_idx, k
     kmax = kv_idx.shape[-1]
     _need(kv_idx, torch.int32, (prob.batch, prob.heads, nb, kmax), "kv_idx")
     _need(kv_count, torch.int32, (prob.batch, prob.heads, nb), "kv_count")
-    out = _out_tensor(prob, q, out)
+    out = _out_tensor(prob, q, out, stream)
     if want_lse and lse is None:
-        lse = torch.empty(shp[:3], dtype=torch.float32, device=q.device)
+        lse = _output(stream, torch.empty, shp[:3], dtype=torch.float32, device=q.device)
     if lse is not None:
         _need(lse, torch.float32, shp[:3], "lse")
     if workspace is None:
-        workspace = torch.empty(remainder_workspace(prob), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(stream, remainder_workspace(prob), q.device)
     ws_min = remainder_workspace(prob, 1)
     if workspace.dtype != torch.uint8 or not workspace.is_cuda or workspace.numel() < ws_min:
         raise ValueError(f"workspace must be a uint8 device tensor of at least {ws_min} bytes")
@@ -485,9 +515,9 @@ def dense_attention(prob: Problem, q, k, v, out=None, want_lse: bool = False, ls
     shp = _qkv_shape(prob)
     for t, n in ((q, "q"), (k, "k"), (v, "v")):
         _need(t, torch.bfloat16, shp, n)
-    out = _out_tensor(prob, q, out)
+    out = _out_tensor(prob, q, out, stream)
     if want_lse and lse is None:
-        lse = torch.empty(shp[:3], dtype=torch.float32, device=q.device)
+        lse = _output(stream, torch.empty, shp[:3], dtype=torch.float32, device=q.device)
     if lse is not None:
         _need(lse, torch.float32, shp[:3], "lse")
     _check(load().sva_dense_attention(ctypes.byref(prob), _ptr(q), _ptr(k), _ptr(v), _ptr(out),
@@ -539,13 +569,13 @@ def quantize_fp8(prob: Problem, q, k, v, out: Optional[dict] = None, stream=None
         nb, npad, dp = num_blocks(prob), fp8_padded_len(prob), fp8_code_dim(prob)
         B, H, D = prob.batch, prob.heads, prob.head_dim
         dev = q.device
-        out = {"q8": torch.empty((B, H, npad, dp), dtype=torch.uint8, device=dev),
-               "k8": torch.empty((B, H, npad, dp), dtype=torch.uint8, device=dev),
-               "v8": torch.empty((B, H, npad // 64, dp, 64), dtype=torch.uint8, device=dev),
-               "q_exp": torch.empty((B, H, nb), dtype=torch.int32, device=dev),
-               "k_exp": torch.empty((B, H, nb), dtype=torch.int32, device=dev),
-               "v_exp": torch.empty((B, H, dp), dtype=torch.int32, device=dev),
-               "k_mean": torch.empty((B, H, D), dtype=torch.bfloat16, device=dev)}
+        out = {"q8": _output(stream, torch.empty, (B, H, npad, dp), dtype=torch.uint8, device=dev),
+               "k8": _output(stream, torch.empty, (B, H, npad, dp), dtype=torch.uint8, device=dev),
+               "v8": _output(stream, torch.empty, (B, H, npad // 64, dp, 64), dtype=torch.uint8, device=dev),
+               "q_exp": _output(stream, torch.empty, (B, H, nb), dtype=torch.int32, device=dev),
+               "k_exp": _output(stream, torch.empty, (B, H, nb), dtype=torch.int32, device=dev),
+               "v_exp": _output(stream, torch.empty, (B, H, dp), dtype=torch.int32, device=dev),
+               "k_mean": _output(stream, torch.empty, (B, H, D), dtype=torch.bfloat16, device=dev)}
     _need_fp8(prob, out, True)
     st = _fp8_struct(out)
     _check(load().sva_quantize_fp8(ctypes.byref(prob), _ptr(q), _ptr(k), _ptr(v), ctypes.byref(st),
@@ -567,10 +597,10 @@ def sparse_attention_fp8(prob: Problem, quant: dict, kv_idx, kv_count, out=None,
     ref = quant["q8"]
     if out is None:
         dt = torch.float32 if prob.out_dtype == SVA_F32 else torch.bfloat16
-        out = torch.empty(shp, dtype=dt, device=ref.device)
+        out = _output(stream, torch.empty, shp, dtype=dt, device=ref.device)
     _need(out, torch.float32 if prob.out_dtype == SVA_F32 else torch.bfloat16, shp, "out")
     if want_lse and lse is None:
-        lse = torch.empty(shp[:3], dtype=torch.float32, device=ref.device)
+        lse = _output(stream, torch.empty, shp[:3], dtype=torch.float32, device=ref.device)
     if lse is not None:
         _need(lse, torch.float32, shp[:3], "lse")
     st = _fp8_struct(quant)
@@ -590,10 +620,10 @@ def dense_attention_fp8(prob: Problem, quant: dict, out=None, want_lse: bool = F
     ref = quant["q8"]
     dt = torch.float32 if prob.out_dtype == SVA_F32 else torch.bfloat16
     if out is None:
-        out = torch.empty(shp, dtype=dt, device=ref.device)
+        out = _output(stream, torch.empty, shp, dtype=dt, device=ref.device)
     _need(out, dt, shp, "out")
     if want_lse and lse is None:
-        lse = torch.empty(shp[:3], dtype=torch.float32, device=ref.device)
+        lse = _output(stream, torch.empty, shp[:3], dtype=torch.float32, device=ref.device)
     if lse is not None:
         _need(lse, torch.float32, shp[:3], "lse")
     st = _fp8_struct(quant)
@@ -638,20 +668,20 @@ def token_select(x, keep_ratio: float, scores=None, kept_idx=None, kept_pos=None
     k = token_keep_count(t, keep_ratio)
     _need(x, torch.bfloat16, (B, N, C), "x")
     if scores is None:
-        scores = torch.empty((B, N), dtype=torch.float64, device=x.device)
+        scores = _output(stream, torch.empty, (B, N), dtype=torch.float64, device=x.device)
     else:
         _need(scores, torch.float64, (B, N), "scores")
     if kept_idx is None:
-        kept_idx = torch.empty((B, k), dtype=torch.int32, device=x.device)
+        kept_idx = _output(stream, torch.empty, (B, k), dtype=torch.int32, device=x.device)
     else:
         _need(kept_idx, torch.int32, (B, k), "kept_idx")
     if kept_pos is None:
-        kept_pos = torch.empty((B, N), dtype=torch.int32, device=x.device)
+        kept_pos = _output(stream, torch.empty, (B, N), dtype=torch.int32, device=x.device)
     else:
         _need(kept_pos, torch.int32, (B, N), "kept_pos")
     ws_bytes = token_select_workspace(t)
     if workspace is None:
-        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device)
+        workspace = _scratch(stream, ws_bytes, x.device)
     if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()
             and workspace.numel() * workspace.element_size() >= ws_bytes):
         raise ValueError(f"workspace must be a contiguous device tensor of >= {ws_bytes} bytes")
@@ -676,15 +706,15 @@ def token_select_noalloc(x, keep_ratio: float, scores=None, kept_idx=None, kept_
     k = token_keep_count(t, keep_ratio)
     _need(x, torch.bfloat16, (B, N, C), "x")
     if scores is None:
-        scores = torch.empty((B, N), dtype=torch.float64, device=x.device)
+        scores = _output(stream, torch.empty, (B, N), dtype=torch.float64, device=x.device)
     else:
         _need(scores, torch.float64, (B, N), "scores")
     if kept_idx is None:
-        kept_idx = torch.empty((B, k), dtype=torch.int32, device=x.device)
+        kept_idx = _output(stream, torch.empty, (B, k), dtype=torch.int32, device=x.device)
     else:
         _need(kept_idx, torch.int32, (B, k), "kept_idx")
     if kept_pos is None:
-        kept_pos = torch.empty((B, N), dtype=torch.int32, device=x.device)
+        kept_pos = _output(stream, torch.empty, (B, N), dtype=torch.int32, device=x.device)
     else:
         _need(kept_pos, torch.int32, (B, N), "kept_pos")
     _check(load().sva_token_select_noalloc(ctypes.byref(t), float(keep_ratio), _ptr(x), _ptr(scores),
@@ -702,7 +732,7 @@ def token_gather(x, kept_idx, x_kept=None, stream=None):
     _need(x, torch.bfloat16, (B, N, C), "x")
     _need(kept_idx, torch.int32, (B, k), "kept_idx")
     if x_kept is None:
-        x_kept = torch.empty((B, k, C), dtype=torch.bfloat16, device=x.device)
+        x_kept = _output(stream, torch.empty, (B, k, C), dtype=torch.bfloat16, device=x.device)
     else:
         _need(x_kept, torch.bfloat16, (B, k, C), "x_kept")
     _check(load().sva_token_gather(ctypes.byref(tokens(B, N, C)), k, _ptr(x), _ptr(kept_idx),
@@ -721,7 +751,7 @@ def token_scatter(y_kept, kept_pos, base, out=None, stream=None):
     _need(kept_pos, torch.int32, (B, N), "kept_pos")
     _need(base, torch.bfloat16, (B, N, C), "base")
     if out is None:
-        out = torch.empty_like(base)
+        out = _output(stream, torch.empty_like, base)
     else:
         _need(out, torch.bfloat16, (B, N, C), "out")
     _check(load().sva_token_scatter(ctypes.byref(tokens(B, N, C)), k, _ptr(y_kept), _ptr(kept_pos),
@@ -874,7 +904,7 @@ def rotary(plan: dict, positions, q, k=None, q_out=None, k_out=None, backward: b
     dev = _on_device(q, "q")
     qi = _heads(q, dt, shp, "q", dev)
     if q_out is None:
-        q_out = torch.empty_like(q)
+        q_out = _output(stream, torch.empty_like, q)
     qo = _heads(q_out, dt, shp, "q_out", dev)
     ki = ko = None
     if k is not None:
@@ -883,7 +913,7 @@ def rotary(plan: dict, positions, q, k=None, q_out=None, k_out=None, backward: b
         shp = (B, k.shape[1], N, D)
         ki = _heads(k, dt, shp, "k", dev)
         if k_out is None:
-            k_out = torch.empty_like(k)
+            k_out = _output(stream, torch.empty_like, k)
         ko = _heads(k_out, dt, shp, "k_out", dev)
     elif k_out is not None:
         raise ValueError("k_out without k")
@@ -971,9 +1001,9 @@ def cache_read(cache: dict, slots, k=None, v=None, dtype="bf16", stream=None) ->
     shp = (B, st.kv_heads, N, st.head_dim)
     ptr, sb = _rows_of_ints(slots, B, N, "slots", dev)
     if k is None:
-        k = torch.empty(shp, dtype=dt, device=slots.device)
+        k = _output(stream, torch.empty, shp, dtype=dt, device=slots.device)
     if v is None:
-        v = torch.empty(shp, dtype=dt, device=slots.device)
+        v = _output(stream, torch.empty, shp, dtype=dt, device=slots.device)
     _check(load().sva_cache_read(st, B, N, code, ptr, sb, _heads(k, dt, shp, "k", dev), _heads(v, dt, shp, "v", dev),
                                  _stream_on(stream, dev)), "sva_cache_read")
     if stream is not None:
@@ -1046,12 +1076,12 @@ def cache_attention(cache: dict, q, page_table, lengths, k_new=None, v_new=None,
         cnt = _plain(counts, i32, (B,), "counts", dev)
     if out is None:
         dt, code = _dtype_code(out_dtype, "out_dtype")
-        out = torch.empty_like(q, dtype=dt)
+        out = _output(stream, torch.empty_like, q, dtype=dt)
     else:
         dt, code = _dtype_code(out.dtype, "out")
     ho = _heads(out, dt, shp, "out", dev)
     if want_lse and lse is None:
-        lse = torch.empty((B, H, T), dtype=torch.float32, device=q.device)
+        lse = _output(stream, torch.empty, (B, H, T), dtype=torch.float32, device=q.device)
     lp = None if lse is None else _plain(lse, torch.float32, (B, H, T), "lse", dev)
     qry = CacheQuery(B, H, T, pages, float(softmax_scale), code)
     lib = load()
@@ -1066,7 +1096,7 @@ def cache_attention(cache: dict, q, page_table, lengths, k_new=None, v_new=None,
                 _workspace_bytes.clear()
             ws_bytes = _workspace_bytes[sizes] = need.value
         if ws_bytes:
-            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            workspace = _scratch(stream, ws_bytes, q.device)
             ws_ptr = workspace.data_ptr()
     else:
         ws_bytes = workspace.numel()
