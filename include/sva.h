@@ -541,7 +541,8 @@ typedef struct sva_cache_query {
                             cache head h / (H / Hkv)                                */
   int32_t queries;       /* T in [1, SVA_CACHE_MAX_QUERIES]                         */
   int32_t max_pages;     /* columns of the page table, >= 1                         */
-  double softmax_scale;  /* c; <= 0 selects 1/sqrt(D)                               */
+  double softmax_scale;  /* c; <= 0 selects 1/sqrt(D); c * log2(e) is used as float32:
+                            what is no normal number there is refused               */
   int32_t out_dtype;     /* sva_dtype of out                                        */
 } sva_cache_query;
 

@@ -1,6 +1,7 @@
 // Host side of the rotary, cache and cache-attention entry points of
 // include/sva.h: argument validation and dispatch.  Every check runs before any
 // HIP call.
+#include <float.h>
 #include <math.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -156,6 +157,8 @@ int check_query(const sva_cache* cache, bool pointers, const sva_cache_query* q,
   if ((int64_t)a->B * cache->kv_heads * (((int64_t)a->G * a->T + 63) / 64) * 16 > INT32_MAX) return SVA_ERR_SHAPE;
   const double c = q->softmax_scale > 0.0 ? q->softmax_scale : 1.0 / sqrt((double)cache->head_dim);
   a->scale_log2 = (float)(c * 1.4426950408889634074);
+  // zero would make a masked key's logit 0 * -inf, infinity every other's
+  if (!(a->scale_log2 >= FLT_MIN && a->scale_log2 <= FLT_MAX)) return SVA_ERR_INVALID_ARG;
   a->out_f32 = q->out_dtype == SVA_F32;
   return SVA_OK;
 }
