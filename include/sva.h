@@ -449,7 +449,7 @@ typedef struct sva_rotary_spec {
 int sva_rotary_frequencies(const sva_rotary_spec* spec, double* freq, double* magnitude);
 
 typedef struct sva_rotary_params {
-  int32_t batch, tokens; /* B >= 1, N >= 1                                          */
+  int32_t batch, tokens; /* B >= 1, N >= 1, B * N <= INT32_MAX                      */
   int32_t head_dim;      /* D in [2, 1024]                                          */
   int32_t rot_dim;       /* even, in [2, min(D, 512)]: the row's first channels     */
   int32_t layout;        /* sva_rotary_layout                                       */
@@ -514,6 +514,7 @@ typedef struct sva_cache {
 } sva_cache;
 
 /* Quantise the rows of N new tokens per batch entry into their slots.
+ *   batch, tokens : B, N >= 1; B * N and B * N / 16 * ceil(Hkv / 4) <= INT32_MAX
  *   dtype : sva_dtype of k and v ([B, Hkv, N, D]; 16-byte aligned data and strides)
  *   slots : int32 device, token (b, n) goes to slots[b * slots_stride_b + n]; a
  *           value outside [0, num_pages * page_size) writes nothing (padding,

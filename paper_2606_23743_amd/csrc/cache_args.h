@@ -7,6 +7,17 @@
 
 namespace sva {
 
+// A dimension of a launch holds fewer than 2^32 threads.  go(first, n) launches workgroups
+// first .. first + n - 1 of `groups`: all of them but for tensors of hundreds of millions of tokens.
+template <class Go>
+void launch_slices(int64_t groups, int threads, Go go) {
+  const int64_t most = UINT32_MAX / threads;
+  for (int64_t first = 0; first < groups; first += most) {
+    const int64_t left = groups - first;
+    go((int)first, (unsigned)(left < most ? left : most));
+  }
+}
+
 struct HeadsView {
   void* p;
   int64_t sb, sh, sn;
@@ -45,6 +56,7 @@ struct CacheRowsArgs {
   int64_t slots_b;
   int B, N;
   bool f32;
+  int first;                     // a launch's first workgroup
 };
 hipError_t launch_cache_write(const CacheRowsArgs& a, hipStream_t stream);
 hipError_t launch_cache_read(const CacheRowsArgs& a, hipStream_t stream);

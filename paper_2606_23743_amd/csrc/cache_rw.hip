@@ -182,7 +182,7 @@ struct Place {
 
   __device__ __forceinline__ Place(const CacheRowsArgs& a) {
     const int groups = (a.c.heads + kHeads - 1) / kHeads;
-    const int wg = xcd_remap(blockIdx.x, gridDim.x);
+    const int wg = a.first + xcd_remap(blockIdx.x, gridDim.x);
     const int tile = wg / groups;
     h0 = (wg - tile * groups) * kHeads;
     const int r = threadIdx.x / TPR;
@@ -325,18 +325,22 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheRowsArgs a) {
 }
 
 template <int D, int FMT, bool F32>
-void launch_one(const CacheRowsArgs& a, bool write, hipStream_t stream) {
+void launch_one(const CacheRowsArgs& args, bool write, hipStream_t stream) {
+  CacheRowsArgs a = args;
   const int64_t tiles = ((int64_t)a.B * a.N + Place<D>::RPP - 1) / Place<D>::RPP;
-  const dim3 grid((unsigned)(tiles * ((a.c.heads + kHeads - 1) / kHeads)), 2);
   constexpr bool kWriteNT = FMT != kCacheBf16 && !F32, kReadNT = F32;
   const bool big = (int64_t)a.B * a.N * a.c.heads * D * (F32 ? 4 : 2) >= (64 << 20);
-  if (write) {
-    if (big) hipLaunchKernelGGL((cache_write_kernel<D, FMT, F32, kWriteNT>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((cache_write_kernel<D, FMT, F32, false>), grid, dim3(kThreads), 0, stream, a);
-  } else {
-    if (big) hipLaunchKernelGGL((cache_read_kernel<D, FMT, F32, kReadNT>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((cache_read_kernel<D, FMT, F32, false>), grid, dim3(kThreads), 0, stream, a);
-  }
+  launch_slices(tiles * ((a.c.heads + kHeads - 1) / kHeads), kThreads, [&](int first, unsigned n) {
+    a.first = first;
+    const dim3 grid(n, 2);
+    if (write) {
+      if (big) hipLaunchKernelGGL((cache_write_kernel<D, FMT, F32, kWriteNT>), grid, dim3(kThreads), 0, stream, a);
+      else hipLaunchKernelGGL((cache_write_kernel<D, FMT, F32, false>), grid, dim3(kThreads), 0, stream, a);
+    } else {
+      if (big) hipLaunchKernelGGL((cache_read_kernel<D, FMT, F32, kReadNT>), grid, dim3(kThreads), 0, stream, a);
+      else hipLaunchKernelGGL((cache_read_kernel<D, FMT, F32, false>), grid, dim3(kThreads), 0, stream, a);
+    }
+  });
 }
 
 template <int D>

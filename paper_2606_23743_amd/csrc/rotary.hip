@@ -33,6 +33,7 @@ struct RotaryGrid {
   int tok, heads;                // tokens and heads of a workgroup
   bool by_head;                  // its items in the order (head, token) instead of (token, head): BY_HEAD
   int rot_items, row_items;      // items of a row that turn, and all of them
+  int first;                     // a launch's first workgroup
 };
 
 // VB bytes at p as dwords: 16, or the largest of 8, 4 and 2 that sizes and strides are multiples of.
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
   __shared__ int64_t base[kMaxTok][4];         // offsets of a token in q_in, q_out, k_in, k_out
 
   const int np = a.rot / 2;
-  const int t0 = blockIdx.x * gr.tok;
+  const int t0 = (gr.first + blockIdx.x) * gr.tok;
   const int nt = min(gr.tok, a.B * a.N - t0);
   if (threadIdx.x < nt) {
     const int b = (t0 + threadIdx.x) / a.N;
@@ -213,11 +214,16 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
 }
 
 template <bool F32, bool HALF, int VB, bool RAGGED, int U>
-void launch_unroll(const RotaryArgs& a, const RotaryGrid& gr, bool nt, hipStream_t stream) {
+void launch_unroll(const RotaryArgs& a, const RotaryGrid& grid, bool nt, hipStream_t stream) {
+  RotaryGrid gr = grid;
   const int64_t tokens = (int64_t)a.B * a.N;
   const int heads = a.qi.heads + a.ki.heads;
-  const dim3 grid((unsigned)((tokens + gr.tok - 1) / gr.tok), (heads + gr.heads - 1) / gr.heads);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a, gr); };
+  auto go = [&](auto kernel) {
+    launch_slices((tokens + gr.tok - 1) / gr.tok, kThreads, [&](int first, unsigned n) {
+      gr.first = first;
+      hipLaunchKernelGGL(kernel, dim3(n, (heads + gr.heads - 1) / gr.heads), dim3(kThreads), 0, stream, a, gr);
+    });
+  };
   constexpr bool NT = VB == 16 && !RAGGED;
   if (gr.by_head && nt) go(rotary_kernel<F32, HALF, VB, RAGGED, U, NT, true>);
   else if (gr.by_head) go(rotary_kernel<F32, HALF, VB, RAGGED, U, false, true>);
@@ -230,7 +236,7 @@ void launch_as(const RotaryArgs& a, hipStream_t stream) {
   constexpr int kItem = F32 ? 4 : 2, E = VB / kItem;
   constexpr bool TWO = HALF || E == 1;
   const int heads = a.qi.heads + a.ki.heads;
-  RotaryGrid gr{1, heads, false, 0, 0};
+  RotaryGrid gr{1, heads, false, 0, 0, 0};
   gr.rot_items = ((TWO ? a.rot / 2 : a.rot) + E - 1) / E;
   gr.row_items = gr.rot_items + (a.copy ? (a.D - a.rot + E - 1) / E : 0);
   // Where a head's tokens lie together (not a token's heads), a workgroup takes 4 KB of each of
