@@ -79,3 +79,37 @@ def test_float32_results_keep_float32_weights(G, T, fmt, D, n):
     err = ce.norm_error(out, want)
     say(f"   error {err:.2e} of the norm, allowed {ce.FINE_NORM:.2e}")
     assert err <= ce.FINE_NORM
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_more_queries_than_a_call_takes_in_parts(causal):
+    """1,300 tokens over a bf16 cache: a prompt's parts attend and are written in turn; a frame's tokens, which all
+    see each other, are written first and attend in parts without drafted keys."""
+    g = np.random.default_rng(9)
+    kv, G, D, N, most, page = 2, 3, 64, 1300, 1024, 32
+    q, k = np.zeros((1, kv * G, N, D)), g.integers(-3, 4, (1, kv, N, D)).astype(np.float64)
+    q[..., 0], k[..., 0] = g.integers(-1, 2, (1, kv * G, N)), g.integers(0, 2, (1, kv, N))
+    v = g.integers(-8, 9, (1, kv, N, D)).astype(np.float64)
+    w = np.exp2(np.einsum("bhtd,bhsd->bhts", q, np.repeat(k, G, 1))) * (np.tri(N) if causal else 1.0)
+    total = w.sum(axis=-1)
+    want = (w @ np.repeat(v, G, 1)) / total[..., None], np.log(total), np.ones((1, kv * G, N), bool)
+    say(f"[cache exact] {N} queries in parts, causal={causal}")
+    dq, dk, dv = (torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16).cuda() for x in (q, k, v))
+    cache = sva.kv_cache(50, kv, D, page, "bf16")
+    table = torch.randperm(50)[:-(-N // page)].to(torch.int32).cuda()[None]
+    at = torch.arange(N, device="cuda")
+    slots = (table[0, at // page] * page + at % page).to(torch.int32)[None]
+    parts = [(a, min(a + most, N)) for a in range(0, N, most)]
+    if not causal:
+        sva.cache_write(cache, dk, dv, slots)
+    out, lse = [], []
+    for a, b in parts:
+        n = torch.tensor([a if causal else N], dtype=torch.int32, device="cuda")
+        new = (dk[:, :, a:b], dv[:, :, a:b]) if causal else ()
+        o, l = sva.cache_attention(cache, dq[:, :, a:b], table, n, *new, softmax_scale=ce.LN2, out_dtype="f32", want_lse=True)
+        if causal:
+            sva.cache_write(cache, *new, slots[:, a:b])
+        out.append(o)
+        lse.append(l)
+    torch.cuda.synchronize()
+    ce.check_whole(torch.cat(out, 2), torch.cat(lse, 2), want, True)

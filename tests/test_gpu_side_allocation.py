@@ -82,3 +82,33 @@ def test_outputs_freed_under_pending_use_are_not_taken():
     torch.cuda.synchronize()
     for got in kept:
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("name", ["cache_attention", "rotary", "cache_read", "token_select"])
+def test_a_side_stream_forked_into_a_capture(name):
+    """Outputs and workspaces allocated on a side stream that takes part in a capture stay the graph's: replays, with
+    eager work between them that allocates, give the eager results."""
+    call = _calls()[name]
+    want = [t.clone() for t in call(None)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    say(f"[side allocation] captured {name}")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = call(side)
+        again = call(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(4):
+        for t in (*got, *again):
+            t.zero_()
+        junk = [torch.full((1 << n,), 0x7F, dtype=torch.uint8, device="cuda") for n in range(16, 27)]
+        eager = call(side)
+        torch.cuda.synchronize()
+        graph.replay()
+        for n in junk:
+            n.fill_(0x55)
+        torch.cuda.synchronize()
+        del junk
+        for result in (got, again, eager):
+            assert all(torch.equal(a, b) for a, b in zip(result, want))
