@@ -533,6 +533,10 @@ int sva_cache_read(const sva_cache* cache, int32_t batch, int32_t tokens, int32_
                    const int32_t* slots, int64_t slots_stride_b, const sva_heads* k,
                    const sva_heads* v, void* stream);
 
+/* Drafted tokens of a call.  A frame or a prompt of more is taken in parts: each part attended with
+ * the ones before it in the cache, and written before the next (what a part sees of the earlier ones is
+ * then rounded to the cache's format); where all tokens of a frame see each other, all are written
+ * first and the queries attend in parts without k_new and v_new.  Each part reads the cache once. */
 #define SVA_CACHE_MAX_QUERIES 1024
 
 /* A step's queries: T drafted tokens per batch entry (one for plain decoding). */

@@ -143,10 +143,11 @@ CacheAttnShape cache_attn_shape(const CacheAttnArgs& a) {
   CacheAttnShape s{};
   const int64_t rows = (int64_t)a.G * a.T;
   // Up to three 16-row tiles each wave holds the state of all rows and has keys of its
-  // own; past that the registers do not, and the waves share keys and divide rows.  us at
-  // two sequences of 223,200 and 8 cache heads, 30 / 48 rows: own keys 165 / 194 (e4m3),
-  // 285 / 310 (bf16); shared 277 / 282, 303 / 345.  At 192 rows of 8 int8 sequences 185 (in
-  // four passes over the keys) against 163.
+  // own; past that the registers do not, and the waves share keys and divide rows.  us, own keys /
+  // shared ones, bf16 results: two sequences of 223,200 and 8 cache heads, 30 rows 191 / 241 (e4m3), 289 / 290
+  // (bf16 cache), 48 rows 199 / 230, 317 / 289; eight of 32,768 and 6 heads, 64 rows (in two passes
+  // over the keys, or one) 203 / 144 (int8), 287 / 148 (bf16), 128 rows 286 / 170, 412 / 179, 192 rows
+  // 362 / 299, 510 / 313.  Float32 results: 48 rows 244 / 280, 313 / 328; 64 rows 233 / 157, 286 / 174.
   s.shared = rows > 48;
   if (s.shared) {
     const int64_t passes = (rows + 127) / 128;     // 128 rows are what a workgroup's registers hold
