@@ -481,6 +481,34 @@ int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* po
                int64_t pos_stride_b, const sva_heads* q_in, const sva_heads* q_out,
                const sva_heads* k_in, const sva_heads* k_out, void* stream);
 
+/* Positions on several axes (time, height, width of a video; an image beside it): token
+ * (b, n)'s position on axis a at data[b * stride_b + n * stride_n + a * stride_a]. */
+#define SVA_ROTARY_MAX_AXES 8
+typedef enum sva_position_type { SVA_POSITIONS_I32 = 0, SVA_POSITIONS_F32 = 1 } sva_position_type;
+typedef struct sva_positions {
+  const void* data;      /* device, 4-byte aligned                                  */
+  int32_t type;          /* sva_position_type: whole, or fractional (seconds, say)  */
+  int32_t axes;          /* in [1, SVA_ROTARY_MAX_AXES]                             */
+  int64_t stride_b, stride_n, stride_a;   /* elements, >= 0; stride_b 0 shares them  */
+} sva_positions;
+
+/* The pairs of `count` axes one after the other: axes[i] gives axis i rot_dim / 2 pairs
+ * with frequencies of their own (base^(-j / that many), scaled as sva_rotary_frequencies
+ * does).  freq (float64) and axis (int32, the axis of each pair): HOST memory for all
+ * pairs, at most 256; the axes' magnitudes must agree.  Equal bases and the sizes (D/2 -
+ * 2*(D/6), D/6, D/6) are what sva_qknorm_rope_pool turns a whole grid by.  Host only. */
+int sva_rotary_axes_frequencies(const sva_rotary_spec* axes, int32_t count, double* freq, int32_t* axis,
+                                double* magnitude);
+
+/* sva_rotary with positions on several axes: pair i turns by t = position[axis[i]] f_i.
+ *   freq : float64 [rot_dim/2] device, 8-byte aligned
+ *   axis : int32 [rot_dim/2] device, in any order; a pair whose axis is none of
+ *          pos->axes has position 0
+ * All else as in sva_rotary, the transposed map and work in place with it. */
+int sva_rotary_axes(const sva_rotary_params* p, const double* freq, const int32_t* axis, const sva_positions* pos,
+                    const sva_heads* q_in, const sva_heads* q_out, const sva_heads* k_in, const sva_heads* k_out,
+                    void* stream);
+
 /* Formats of a cache.  One scale per token and head, apart for K and V: an
  * element is its code times its row's scale.  With a the row's largest
  * magnitude:
@@ -598,6 +626,107 @@ int sva_cache_attention(const sva_cache* cache, const sva_cache_query* query, co
                         const sva_heads* v_new, const uint8_t* mask, int64_t mask_stride_b,
                         const int32_t* counts, void* workspace, size_t workspace_bytes,
                         const sva_heads* out, float* lse, void* stream);
+
+/* ---- Around self-attention in a denoiser's layer: layer norm and cross attention to an
+ * encoder's states, each with its gradients. ---- */
+
+/* Rows [B, N, C]: element (b, n, c) at data + b*stride_b + n*stride_n + c, strides in
+ * elements, >= 0.  An input may repeat itself (stride 0); an output's rows must not
+ * overlap. */
+typedef struct sva_rows {
+  void* data;
+  int64_t stride_b, stride_n;
+} sva_rows;
+
+typedef struct sva_layer_norm_params {
+  int32_t batch, tokens;   /* B, N >= 1, B * N <= INT32_MAX - 2^20                  */
+  int32_t channels;        /* C in [1, 16384]                                       */
+  int32_t dtype;           /* sva_dtype of x, y and their gradients                 */
+  int32_t weight_dtype;    /* sva_dtype of weight and bias                          */
+  int32_t per_entry;       /* nonzero: weight and bias are [B, C], a row per batch
+                              entry (adaptive norm); else [C]                       */
+  int32_t unit_offset;     /* nonzero: the factor is 1 + weight                     */
+  int64_t weight_stride_b; /* per_entry: elements between entries' rows, >= 0       */
+  int64_t bias_stride_b;
+  double eps;              /* finite, a normal float32 > 0                          */
+} sva_layer_norm_params;
+
+/* y = (x - mean) rstd w + bias, rstd = 1 / sqrt(var + eps), over a row's C channels (var
+ * without Bessel's correction).
+ *   weight, bias : device, aligned to their elements, or NULL (ones, zeros)
+ *   y            : may be x (same data and strides), must otherwise lie apart from it
+ *   mean, rstd   : float32 [B, N] device, written, or NULL; what the gradient needs
+ * Data aligned to their elements; accesses are of whole 16 bytes where data and strides
+ * are multiples of 16 bytes and C of 8.  Sums are float32, squares are of deviations from
+ * the mean; y is rounded once. */
+int sva_layer_norm(const sva_layer_norm_params* p, const sva_rows* x, const void* weight, const void* bias,
+                   const sva_rows* y, float* mean, float* rstd, void* stream);
+
+/* Bytes of device workspace for the weights' gradients (for any strides of these sizes).
+ * Host only. */
+int sva_layer_norm_backward_workspace(const sva_layer_norm_params* p, size_t* bytes);
+
+/* Gradients: with xhat = (x - mean) rstd and g = dy w,
+ *   dx      = rstd (g - mean(g) - xhat mean(g xhat))
+ *   dweight = sum of dy xhat, dbias = sum of dy: over all rows float32 [C], or with
+ *             per_entry over an entry's [B, C]; contiguous; either may be NULL
+ *   dx may be dy or x (same data and strides), must otherwise lie apart from both
+ *   mean, rstd : float32 [B, N], as sva_layer_norm wrote them
+ *   workspace  : 256-byte aligned, at least sva_layer_norm_backward_workspace bytes; not
+ *                read where neither sum is wanted.  Calls that share one must not overlap.
+ * Sums are float32 in a fixed order: the same call gives the same bits. */
+int sva_layer_norm_backward(const sva_layer_norm_params* p, const sva_rows* dy, const sva_rows* x, const void* weight,
+                            const float* mean, const float* rstd, void* workspace, size_t workspace_bytes,
+                            const sva_rows* dx, float* dweight, float* dbias, void* stream);
+
+/* Cross attention: N query tokens, M states of an encoder. */
+typedef struct sva_cross {
+  int32_t batch;         /* B >= 1                                                  */
+  int32_t heads;         /* H, a multiple of kv_heads; head h reads h / (H / Hkv)   */
+  int32_t kv_heads;      /* Hkv >= 1                                                */
+  int32_t queries;       /* N >= 1; B * H * N <= INT32_MAX - 2^16                   */
+  int32_t keys;          /* M >= 1; B * Hkv * M <= INT32_MAX - 2^16                 */
+  int32_t head_dim;      /* D in {64, 112, 128}                                     */
+  double softmax_scale;  /* c; <= 0 selects 1/sqrt(D); what is no normal number as a
+                            float32 (c, c * log2(e)) is refused                     */
+} sva_cross;
+
+/* Bytes of device workspace of the two calls below (masked: with a mask): lists of keys,
+ * and partial results where few rows meet many keys (or few keys many rows).  Host
+ * only. */
+int sva_cross_attention_workspace(const sva_cross* p, int32_t masked, size_t* bytes);
+int sva_cross_attention_backward_workspace(const sva_cross* p, int32_t masked, size_t* bytes);
+
+/* out = softmax(c Q K^T) V over the keys that an entry has.
+ *   q, out  : bf16 [B, H, N, D]; out apart from every input
+ *   k, v    : bf16 [B, Hkv, M, D]
+ *   lengths : int32 [B] device or NULL (M): keys 0 .. lengths[b]-1, clamped to [0, M]
+ *   mask    : uint8 device or NULL: key m of entry b is seen where mask[b * mask_stride_b
+ *             + m] != 0 (mask_stride_b 0 shares one); with lengths, both must allow a key
+ *   lse     : float32 [B, H, N] contiguous or NULL: natural-log log-sum-exp of the scaled
+ *             logits
+ *   workspace : 256-byte aligned, may be NULL where none is needed; contents on entry do
+ *             not matter.  Calls that share one must not overlap.
+ * Tensors by strides, 16-byte aligned data and strides.  Hidden keys and values take no
+ * part, whatever they hold; a query of an entry without keys gets zeros and an lse of
+ * -inf.  Products are bf16 MFMA with float32 accumulation; weights are rounded to bf16
+ * for the product with V and divided by their sum as rounded, lse is of the unrounded
+ * ones.  The same call gives the same bits. */
+int sva_cross_attention(const sva_cross* p, const sva_heads* q, const sva_heads* k, const sva_heads* v,
+                        const int32_t* lengths, const uint8_t* mask, int64_t mask_stride_b, void* workspace,
+                        size_t workspace_bytes, const sva_heads* out, float* lse, void* stream);
+
+/* Gradients of q, k and v from dout, the gradient of out, with out and lse as
+ * sva_cross_attention wrote them for the same arguments.
+ *   dout, dq : bf16 [B, H, N, D]; dk, dv: bf16 [B, Hkv, M, D], summed over a group's heads
+ *   dq, dk and dv lie apart from each other and from every input; hidden keys' rows of dk
+ *   and dv are written with zeros, and rows of dq of an entry without keys
+ * Weights and their gradients are rounded to bf16 for their products, sums are float32,
+ * results are rounded once.  The same call gives the same bits. */
+int sva_cross_attention_backward(const sva_cross* p, const sva_heads* dout, const sva_heads* q, const sva_heads* k,
+                                 const sva_heads* v, const sva_heads* out, const float* lse, const int32_t* lengths,
+                                 const uint8_t* mask, int64_t mask_stride_b, void* workspace, size_t workspace_bytes,
+                                 const sva_heads* dq, const sva_heads* dk, const sva_heads* dv, void* stream);
 
 /* Static text for a status code. */
 const char* sva_status_string(int status);

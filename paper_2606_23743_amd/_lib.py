@@ -24,6 +24,8 @@ SVA_SELECT_TOPK, SVA_SELECT_CUMMASS = 0, 1
 SVA_SELECT_MAX_BLOCKS = 2048
 SVA_ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 SVA_ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+SVA_ROTARY_MAX_AXES = 8
+SVA_POSITIONS_I32, SVA_POSITIONS_F32 = 0, 1
 SVA_CACHE_FORMATS = {"bf16": 0, "e4m3": 1, "int8": 2}
 SVA_CACHE_MAX_QUERIES = 1024
 
@@ -89,6 +91,28 @@ class CacheQuery(ctypes.Structure):
                 ("max_pages", ctypes.c_int32), ("softmax_scale", ctypes.c_double), ("out_dtype", ctypes.c_int32)]
 
 
+class Positions(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64), ("stride_a", ctypes.c_int64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+
+
+class LayerNormParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("per_entry", ctypes.c_int32),
+                ("unit_offset", ctypes.c_int32), ("weight_stride_b", ctypes.c_int64),
+                ("bias_stride_b", ctypes.c_int64), ("eps", ctypes.c_double)]
+
+
+class Cross(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("queries", ctypes.c_int32), ("keys", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_double)]
+
+
 _lib = None
 
 
@@ -105,6 +129,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     P, S = ctypes.POINTER(Problem), ctypes.POINTER(SelectParams)
     vp, i32p = ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32)
     i32, i64, HP, CP = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(Heads), ctypes.POINTER(Cache)
+    NP, RP, XP = ctypes.POINTER(LayerNormParams), ctypes.POINTER(Rows), ctypes.POINTER(Cross)
     sig = {
         "sva_num_blocks": [P, i32p],
         "sva_max_keep": [P, S, i32p],
@@ -138,6 +163,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "sva_cache_attention_workspace": [CP, ctypes.POINTER(CacheQuery), ctypes.POINTER(ctypes.c_size_t)],
         "sva_cache_attention": [CP, ctypes.POINTER(CacheQuery), HP, vp, vp, HP, HP, vp, i64, vp, vp,
                                 ctypes.c_size_t, HP, vp, vp],
+        "sva_rotary_axes_frequencies": [ctypes.POINTER(RotarySpec), i32, ctypes.POINTER(ctypes.c_double), i32p,
+                                        ctypes.POINTER(ctypes.c_double)],
+        "sva_rotary_axes": [ctypes.POINTER(RotaryParams), vp, vp, ctypes.POINTER(Positions), HP, HP, HP, HP, vp],
+        "sva_layer_norm": [NP, RP, vp, vp, RP, vp, vp, vp],
+        "sva_layer_norm_backward_workspace": [NP, ctypes.POINTER(ctypes.c_size_t)],
+        "sva_layer_norm_backward": [NP, RP, RP, vp, vp, vp, vp, ctypes.c_size_t, RP, vp, vp, vp],
+        "sva_cross_attention_workspace": [XP, i32, ctypes.POINTER(ctypes.c_size_t)],
+        "sva_cross_attention_backward_workspace": [XP, i32, ctypes.POINTER(ctypes.c_size_t)],
+        "sva_cross_attention": [XP, HP, HP, HP, vp, vp, i64, vp, ctypes.c_size_t, HP, vp, vp],
+        "sva_cross_attention_backward": [XP, HP, HP, HP, HP, HP, vp, vp, vp, i64, vp, ctypes.c_size_t, HP, HP, HP, vp],
         "sva_status_string": [ctypes.c_int],
         "sva_version": [],
     }
@@ -893,6 +928,17 @@ def rotary(plan: dict, positions, q, k=None, q_out=None, k_out=None, backward: b
     for all entries.  q_out / k_out may be q / k (in place).  backward: the
     transposed map, from gradients of the outputs to gradients of the inputs.
     Returns (q_out, k_out), k_out None without k."""
+    dev, prm, q_out, k_out, (qi, qo, ki, ko) = _rotary_tensors(plan, q, k, q_out, k_out, backward, stream)
+    freq = plan["freq"]
+    pos, pos_b = _rows_of_ints(positions, prm.batch, prm.tokens, "positions", dev)
+    _check(load().sva_rotary(prm, _plain(freq, _torch().float64, (prm.rot_dim // 2,), "plan['freq']", dev), pos, pos_b, qi,
+                             qo, ki, ko, _stream_on(stream, dev)), "sva_rotary")
+    _record(stream, q, k, q_out, k_out, freq, positions)
+    return q_out, k_out
+
+
+def _rotary_tensors(plan, q, k, q_out, k_out, backward, stream):
+    """The tensors of a rotary call: device, parameters, outputs and their views."""
     torch = _torch()
     if not isinstance(q, torch.Tensor) or q.dim() != 4:
         raise ValueError("q must be a tensor [B, H, N, D]")
@@ -917,13 +963,9 @@ def rotary(plan: dict, positions, q, k=None, q_out=None, k_out=None, backward: b
         ko = _heads(k_out, dt, shp, "k_out", dev)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    freq, rot = plan["freq"], plan["rot_dim"]
-    pos, pos_b = _rows_of_ints(positions, B, N, "positions", dev)
-    prm = RotaryParams(B, N, D, rot, SVA_ROTARY_LAYOUTS[plan["layout"]], code, 1 if backward else 0, plan["magnitude"])
-    _check(load().sva_rotary(prm, _plain(freq, torch.float64, (rot // 2,), "plan['freq']", dev), pos, pos_b, qi, qo, ki,
-                             ko, _stream_on(stream, dev)), "sva_rotary")
-    _record(stream, q, k, q_out, k_out, freq, positions)
-    return q_out, k_out
+    prm = RotaryParams(B, N, D, plan["rot_dim"], SVA_ROTARY_LAYOUTS[plan["layout"]], code, 1 if backward else 0,
+                       plan["magnitude"])
+    return dev, prm, q_out, k_out, (qi, qo, ki, ko)
 
 
 def kv_cache(num_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, fmt: str = "e4m3",

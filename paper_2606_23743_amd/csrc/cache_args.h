@@ -30,6 +30,10 @@ struct RotaryArgs {
   const double* freq;
   const int32_t* pos;
   int64_t pos_b;
+  const int32_t* axis;           // several axes: of each pair; null: one, position n of an entry at pos[n]
+  int64_t pos_n, pos_a;          // several axes: strides of tokens and axes
+  int axes;
+  bool pos_f32;                  // several axes: positions are float32
   int B, N, D, rot;
   float magnitude;
   bool f32, half, backward;

@@ -1,0 +1,403 @@
+// Gradients of cross attention.  With P = exp(c s - lse), dO the gradient of O and
+// delta = rowsum(dO O):
+//   dV = P^T dO, dP = dO V^T, dS = P (dP - delta), dQ = c dS K, dK = c dS^T Q.
+//
+// Two launches, so that no sum goes through atomics and the same call gives the same
+// bits; S and dP are formed in both (seven products where five would do, against
+// partial dQ of every key tile through memory).
+//   rows: a workgroup holds 128 (64) rows, as the forward kernel does, with Q and dO
+//     in registers, and walks the keys; P and dS stay in registers and are the operand
+//     of dQ^T += K^T dS^T as they stand.  It also forms delta, which the second launch
+//     reads.
+//   keys: a workgroup holds 128 keys (32 a wave) with K and V in registers and walks
+//     the rows of all heads of the group, so dK and dV are summed over them where they
+//     are; S = Q K^T here has the rows in the registers and a key in every lane, P and
+//     dS are again operands as they stand.  The walk is divided among workgroups where
+//     keys are few, and the parts are added in order by a third launch.
+// P and dS are rounded to bf16 once, for their products; everything else is float32.
+#include "cross_tiles.h"
+
+namespace sva {
+namespace {
+
+using namespace cross;
+
+constexpr int NST = 4, PD = 3;   // LDS stages, tiles ahead
+
+template <int D, int QT, bool GATHER>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, QT == 2 ? 2 : 4)))
+void cross_grad_rows_kernel(CrossArgs a) {
+  using G16 = Geo16<D>;
+  using Loader = TileLoader<D>;
+  constexpr int CT = Loader::CT, NUW = Loader::NUW;
+  __shared__ __attribute__((aligned(1024))) unsigned char Ks[NST][CT];
+  __shared__ __attribute__((aligned(1024))) unsigned char Vs[NST][CT];
+  __shared__ int ring[GATHER ? RowRing::kSize : 1];
+
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int id = __builtin_amdgcn_readfirstlane(xcd_remap(blockIdx.x, a.wgs));
+  const int per = a.tiles * a.splits, bh = id / per, rest = id - bh * per;
+  const int split = rest / a.tiles, tile = rest - split * a.tiles;
+  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+
+  const int count = seen_keys_of_all(a, b);
+  const int chunks_all = (count + CK - 1) / CK;
+  const int c0 = (int)((int64_t)chunks_all * split / a.splits), c1 = (int)((int64_t)chunks_all * (split + 1) / a.splits);
+  const int chunks = c1 - c0;
+
+  const int row0 = tile * 64 * QT + w * 16 * QT;
+  const uint16_t* Kh = static_cast<const uint16_t*>(a.k.p) + b * a.k.sb + kvh * a.k.sh;
+  const uint16_t* Vh = static_cast<const uint16_t*>(a.v.p) + b * a.v.sb + kvh * a.v.sh;
+  const float sl2 = a.scale_log2;
+
+  Loader ld;
+  ld.init(w, lane);
+  const unsigned ks_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Ks[0][0]);
+  const unsigned vs_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Vs[0][0]);
+  RowRing rr{ring, GATHER ? a.rows + (int64_t)b * a.M : nullptr, count};
+  auto fetch = [&](int st, int c) {
+    const int first = (c0 + c) * CK, end = c < chunks ? count : 0;
+    if constexpr (GATHER) {
+      int list[NUW];
+#pragma unroll
+      for (int u = 0; u < NUW; ++u) list[u] = c < chunks ? rr.at(first + ld.row[u]) : 0;
+      ld.load_rows(Kh, a.k.sn, list, end - first, ks_base + st * CT);
+      ld.load_rows(Vh, a.v.sn, list, end - first, vs_base + st * CT);
+    } else {
+      ld.load(Kh, a.k.sn, first, end, ks_base + st * CT);
+      ld.load(Vh, a.v.sn, first, end, vs_base + st * CT);
+    }
+  };
+
+  // Q and dO of the wave's rows, their lse and delta
+  bf16x8 qop[QT][G16::KS], gop[QT][G16::KS];
+  float lse2[QT], delta[QT];
+  {
+    const uint16_t *qrow[QT], *grow[QT], *orow[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      const int r = row0 + qt * 16 + i;
+      const bool there = r < a.R;
+      const int rr_ = there ? r : 0;
+      qrow[qt] = there ? static_cast<const uint16_t*>(a.q.p) + row_offset(a.q, b, kvh * a.G, rr_, a.N) : nullptr;
+      grow[qt] = there ? static_cast<const uint16_t*>(a.dout.p) + row_offset(a.dout, b, kvh * a.G, rr_, a.N) : nullptr;
+      orow[qt] = there ? static_cast<const uint16_t*>(a.out.p) + row_offset(a.out, b, kvh * a.G, rr_, a.N) : nullptr;
+      // a row that saw no key has P = 0 everywhere
+      const float lse = there ? a.lse[(int64_t)bh * a.R + rr_] : -INFINITY;
+      lse2[qt] = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634074f;
+    }
+    bf16x8 oop[QT][G16::KS];
+    load_operand<D>(qop, qrow, lane);
+    load_operand<D>(gop, grow, lane);
+    load_operand<D>(oop, orow, lane);
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      float s = 0.0f;
+#pragma unroll
+      for (int x = 0; x < G16::KS; ++x)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf((float)gop[qt][x][e], (float)oop[qt][x][e], s);
+      delta[qt] = quad_sum(s);
+      const int r = row0 + qt * 16 + i;
+      if (split == 0 && g == 0 && r < a.R) a.stat[(int64_t)bh * a.R + r] = make_float2(lse2[qt], delta[qt]);
+    }
+  }
+
+  int koff[G16::KS], voff[G16::DT];
+  operand_offsets<D>(lane, koff, voff);
+  f32x4 dq[G16::DT][QT] = {};
+  if (chunks > 0) {
+    if constexpr (GATHER) {
+      rr.fill(c0 * CK);
+      rr.fill(c0 * CK + RowRing::kHalf);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int c = 0; c < PD; ++c) fetch(c, c);
+    int st = 0;
+#pragma unroll 1
+    for (int c = 0; c < chunks; ++c) {
+      wait_vmcnt_lds_idle<2 * NUW * (PD - 1)>();     // tile c has landed
+      wg_barrier();                                  // and every wave is done with tile c - 1
+      if constexpr (GATHER) {
+        if (c != 0 && c % (RowRing::kHalf / CK) == 0) rr.fill(c0 * CK + c * CK + RowRing::kHalf);
+      }
+      fetch((st + PD) % NST, c + PD);
+      const unsigned char *kt = &Ks[0][0] + st * CT, *vt = &Vs[0][0] + st * CT;
+      f32x4 s[2][QT], dp[2][QT];
+      qk16<D>(s, kt, koff, qop);
+      qk16<D>(dp, vt, koff, gop);
+      const int left = __builtin_amdgcn_readfirstlane(count - (c0 + c) * CK);
+      if (__builtin_expect(left < CK, 0)) {
+        asm volatile("");
+        mask_tail16(s, left, lane);
+      }
+      bf16x8 dsop[QT];
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        u32x4 wv;
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e], sl2, -lse2[qt]));
+            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e + 1], sl2, -lse2[qt]));
+            const bf16x2 x = cvt2(p0 * (dp[k2][qt][2 * e] - delta[qt]), p1 * (dp[k2][qt][2 * e + 1] - delta[qt]));
+            wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, x);
+          }
+        dsop[qt] = __builtin_bit_cast(bf16x8, wv);
+      }
+      pv16<D>(dsop, kt, voff, dq);
+      st = (st + 1) % NST;
+    }
+    wait_vmcnt<0>();               // no load may still target this workgroup's LDS
+  }
+
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int r = row0 + qt * 16 + i;
+    if (r >= a.R) continue;
+    if (a.splits > 1) {
+      float* o = a.part + (((int64_t)bh * a.splits + split) * a.R + r) * D;
+#pragma unroll
+      for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = dq[dt][qt];
+      continue;
+    }
+    uint16_t* o = static_cast<uint16_t*>(a.dq.p) + row_offset(a.dq, b, kvh * a.G, r, a.N);
+#pragma unroll
+    for (int dt = 0; dt < G16::DT; ++dt) {
+      const bf16x2 x = cvt2(dq[dt][qt][0] * a.scale, dq[dt][qt][1] * a.scale);
+      const bf16x2 y = cvt2(dq[dt][qt][2] * a.scale, dq[dt][qt][3] * a.scale);
+      const bf16x4 z = {x[0], x[1], y[0], y[1]};
+      *reinterpret_cast<bf16x4*>(o + dt * 16 + 4 * g) = z;
+    }
+  }
+}
+
+template <int D, bool GATHER>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void cross_grad_keys_kernel(CrossArgs a) {
+  using G16 = Geo16<D>;
+  using Loader = TileLoader<D>;
+  constexpr int CT = Loader::CT, NUW = Loader::NUW, KT = 2;
+  constexpr int kLoads = 2 * NUW + 1;            // of a wave for a tile: Q, dO, statistics
+  __shared__ __attribute__((aligned(1024))) unsigned char Qs[NST][CT];
+  __shared__ __attribute__((aligned(1024))) unsigned char Gs[NST][CT];
+  __shared__ __attribute__((aligned(256))) float2 Ss[NST][CK];
+
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // (kv head of an entry, part of the rows, key tile)
+  const int id = __builtin_amdgcn_readfirstlane(xcd_remap(blockIdx.x, a.kv_wgs));
+  const int per = a.key_tiles * a.row_splits, bh = id / per, rest = id - bh * per;
+  const int split = rest / a.key_tiles, tile = rest - split * a.key_tiles;
+  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+  const int count = seen_keys_of_all(a, b);
+  const int key0 = tile * 128 + w * 32;
+  const int32_t* list = GATHER ? a.rows + (int64_t)b * a.M : nullptr;
+  const float sl2 = a.scale_log2;
+
+  f32x4 dk[G16::DT][KT] = {}, dv[G16::DT][KT] = {};
+  if (tile * 128 < count) {
+    bf16x8 kop[KT][G16::KS], vop[KT][G16::KS];
+    {
+      const uint16_t *krow[KT], *vrow[KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const int j = key0 + kt * 16 + i;
+        krow[kt] = vrow[kt] = nullptr;
+        if (j < count) {
+          const int64_t key = GATHER ? list[j] : j;
+          krow[kt] = static_cast<const uint16_t*>(a.k.p) + b * a.k.sb + kvh * a.k.sh + key * a.k.sn;
+          vrow[kt] = static_cast<const uint16_t*>(a.v.p) + b * a.v.sb + kvh * a.v.sh + key * a.v.sn;
+        }
+      }
+      load_operand<D>(kop, krow, lane);
+      load_operand<D>(vop, vrow, lane);
+    }
+
+    // The walk: tiles of 32 tokens of the group's first head, then of the next.
+    const int per_head = (a.N + CK - 1) / CK;
+    const int64_t all = (int64_t)per_head * a.G;
+    const int64_t t0 = all * split / a.row_splits, t1 = all * (split + 1) / a.row_splits;
+    Loader ld;
+    ld.init(w, lane);
+    const unsigned qs_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Qs[0][0]);
+    const unsigned gs_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Gs[0][0]);
+    const unsigned ss_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Ss[0][0]);
+    int64_t ft = t0;                             // the next tile to load
+    int fh = (int)(t0 / per_head), fn = (int)(t0 - (int64_t)fh * per_head) * CK;
+    auto fetch = [&](int st) {
+      const int end = ft < t1 ? a.N : 0;
+      const int64_t h = kvh * a.G + (ft < t1 ? fh : 0);
+      ld.load(static_cast<const uint16_t*>(a.q.p) + b * a.q.sb + h * a.q.sh, a.q.sn, fn, end, qs_base + st * CT);
+      ld.load(static_cast<const uint16_t*>(a.dout.p) + b * a.dout.sb + h * a.dout.sh, a.dout.sn, fn, end, gs_base + st * CT);
+      const float* from = reinterpret_cast<const float*>(a.stat + ((int64_t)b * a.H + h) * a.N + fn) + lane;
+      global_to_lds<4>(fn + lane / 2 < end ? from : kInf + (lane & 1), ss_base + st * (int)(CK * sizeof(float2)));
+      ++ft;
+      fn += CK;
+      if (fn >= a.N) {
+        fn = 0;
+        ++fh;
+      }
+    };
+    int koff[G16::KS], voff[G16::DT];
+    operand_offsets<D>(lane, koff, voff);
+#pragma unroll
+    for (int c = 0; c < PD; ++c) fetch(c);
+    int st = 0;
+#pragma unroll 1
+    for (int64_t t = t0; t < t1; ++t) {
+      wait_vmcnt_lds_idle<kLoads * (PD - 1)>();      // this tile has landed
+      wg_barrier();                                  // and every wave is done with the one before
+      fetch((st + PD) % NST);
+      if (key0 < count) {
+        const unsigned char *qt = &Qs[0][0] + st * CT, *gt = &Gs[0][0] + st * CT;
+        const float4* stat = reinterpret_cast<const float4*>(&Ss[st][0]);   // rows 2x and 2x + 1
+        f32x4 s[2][KT], dp[2][KT];
+        qk16<D>(s, qt, koff, kop);
+        qk16<D>(dp, gt, koff, vop);
+        bf16x8 pop[KT], dsop[KT];
+        u32x4 pw[KT], dw[KT];
+#pragma unroll
+        for (int r2 = 0; r2 < 2; ++r2)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float4 x = stat[r2 * 8 + 2 * g + e];     // (lse, delta) of two rows
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r2][kt][2 * e], sl2, -x.x));
+              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r2][kt][2 * e + 1], sl2, -x.z));
+              const bf16x2 p = cvt2(p0, p1);
+              const bf16x2 d = cvt2(p0 * (dp[r2][kt][2 * e] - x.y), p1 * (dp[r2][kt][2 * e + 1] - x.w));
+              pw[kt][r2 * 2 + e] = __builtin_bit_cast(unsigned, p);
+              dw[kt][r2 * 2 + e] = __builtin_bit_cast(unsigned, d);
+            }
+          }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+          pop[kt] = __builtin_bit_cast(bf16x8, pw[kt]);
+          dsop[kt] = __builtin_bit_cast(bf16x8, dw[kt]);
+        }
+        pv16<D>(pop, gt, voff, dv);
+        pv16<D>(dsop, qt, voff, dk);
+      }
+      st = (st + 1) % NST;
+    }
+    wait_vmcnt<0>();               // no load may still target this workgroup's LDS
+  }
+
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const int j = key0 + kt * 16 + i;
+    if (j >= a.M) continue;
+    if (a.row_splits > 1) {
+      if (j >= count) continue;                  // the join knows which are hidden
+      float* k = a.part_kv + ((((int64_t)bh * a.row_splits + split) * 2) * a.M + j) * D;
+      float* v = k + (int64_t)a.M * D;
+#pragma unroll
+      for (int dt = 0; dt < G16::DT; ++dt) {
+        *reinterpret_cast<f32x4*>(k + dt * 16 + 4 * g) = dk[dt][kt];
+        *reinterpret_cast<f32x4*>(v + dt * 16 + 4 * g) = dv[dt][kt];
+      }
+      continue;
+    }
+    const bool there = j < count;
+    const int64_t key = GATHER ? list[j] : j;
+    uint16_t* k = static_cast<uint16_t*>(a.dk.p) + b * a.dk.sb + kvh * a.dk.sh + key * a.dk.sn;
+    uint16_t* v = static_cast<uint16_t*>(a.dv.p) + b * a.dv.sb + kvh * a.dv.sh + key * a.dv.sn;
+#pragma unroll
+    for (int dt = 0; dt < G16::DT; ++dt) {
+      const bf16x2 x = cvt2(dk[dt][kt][0] * a.scale, dk[dt][kt][1] * a.scale);
+      const bf16x2 y = cvt2(dk[dt][kt][2] * a.scale, dk[dt][kt][3] * a.scale);
+      const bf16x2 p = cvt2(dv[dt][kt][0], dv[dt][kt][1]), q = cvt2(dv[dt][kt][2], dv[dt][kt][3]);
+      const bf16x4 none = {};
+      const bf16x4 kz = {x[0], x[1], y[0], y[1]}, vz = {p[0], p[1], q[0], q[1]};
+      *reinterpret_cast<bf16x4*>(k + dt * 16 + 4 * g) = there ? kz : none;
+      *reinterpret_cast<bf16x4*>(v + dt * 16 + 4 * g) = there ? vz : none;
+    }
+  }
+}
+
+// Adds the parts of dQ (which 0) or of dK and dV (1, 2) in their order, four channels a
+// lane; a hidden key's gradients are zeros.
+template <int D>
+__global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossArgs a, int first) {
+  constexpr int kLanes = D / 4, kRows = kThreads / kLanes;
+  const int which = first + blockIdx.y, c = threadIdx.x % kLanes * 4;
+  const int rows = which == 0 ? a.R : a.M, parts = which == 0 ? a.splits : a.row_splits;
+  const int64_t at = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
+  if (threadIdx.x >= kRows * kLanes || at >= (int64_t)a.B * a.Hkv * rows) return;
+  const int bh = (int)(at / rows), r = (int)(at - (int64_t)bh * rows);
+  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
+  f32x4 s = {};
+  if (which == 0 || r < seen_keys(a, b)) {
+    const float* from = which == 0 ? a.part + ((int64_t)bh * parts * rows + r) * D + c
+                                   : a.part_kv + (((int64_t)bh * parts * 2 + (which - 1)) * rows + r) * D + c;
+    const int64_t step = (int64_t)rows * D * (which == 0 ? 1 : 2);
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) s += *reinterpret_cast<const f32x4*>(from + p * step);
+  }
+  const float f = which == 2 ? 1.0f : a.scale;
+  const bf16x2 x = cvt2(s[0] * f, s[1] * f), y = cvt2(s[2] * f, s[3] * f);
+  const bf16x4 z = {x[0], x[1], y[0], y[1]};
+  int64_t off;
+  const HeadsView& to = which == 0 ? a.dq : which == 1 ? a.dk : a.dv;
+  if (which == 0) off = row_offset(to, b, kvh * a.G, r, a.N);
+  else off = b * to.sb + kvh * to.sh + (int64_t)(a.mask ? a.rows[(int64_t)b * a.M + r] : r) * to.sn;
+  *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(to.p) + off + c) = z;
+}
+
+template <int D>
+void launch_d(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
+  auto go = [&](auto kernel, int wgs) { hipLaunchKernelGGL(kernel, dim3(wgs), dim3(kThreads), 0, stream, a); };
+  if (s.narrow && a.mask) go(cross_grad_rows_kernel<D, 1, true>, a.wgs);
+  else if (s.narrow) go(cross_grad_rows_kernel<D, 1, false>, a.wgs);
+  else if (a.mask) go(cross_grad_rows_kernel<D, 2, true>, a.wgs);
+  else go(cross_grad_rows_kernel<D, 2, false>, a.wgs);
+  if (a.mask) go(cross_grad_keys_kernel<D, true>, a.kv_wgs);
+  else go(cross_grad_keys_kernel<D, false>, a.kv_wgs);
+  auto sum = [&](int first, int n, int64_t rows) {
+    constexpr int kRows = kThreads / (D / 4);
+    hipLaunchKernelGGL(cross_sum_kernel<D>, dim3((unsigned)((rows + kRows - 1) / kRows), n), dim3(kThreads), 0, stream, a, first);
+  };
+  if (a.splits > 1) sum(0, 1, (int64_t)a.B * a.Hkv * a.R);
+  if (a.row_splits > 1) sum(1, 2, (int64_t)a.B * a.Hkv * a.M);
+}
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+CrossShape cross_grad_shape(int B, int Hkv, int G, int N, int M, int D, bool mask) {
+  CrossShape s = cross_shape(B, Hkv, G, N, M, D, mask);
+  const int64_t heads = (int64_t)B * Hkv, R = (int64_t)G * N;
+  s.key_tiles = (M + 127) / 128;
+  const int64_t base = heads * s.key_tiles, walk = (((int64_t)N + 31) / 32 * G + 7) / 8;
+  int64_t parts = base < 1024 ? 1024 / base : 1;
+  if (parts > walk) parts = walk;
+  s.row_splits = (int)parts;
+  size_t at = mask ? s.seen_at + up256((size_t)B * 4) : 0;
+  s.stat_at = at;
+  at += up256((size_t)heads * R * 8);
+  s.part_at = at;
+  if (s.splits > 1) at += up256((size_t)heads * s.splits * R * D * 4);
+  s.part_kv_at = at;
+  if (s.row_splits > 1) at += up256((size_t)heads * s.row_splits * 2 * M * D * 4);
+  s.ws_bytes = at;
+  return s;
+}
+
+hipError_t launch_cross_attention_grad(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
+  if (a.mask) {
+    const hipError_t e = launch_cross_rows(a, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (a.D == 64) launch_d<64>(a, s, stream);
+  else if (a.D == 112) launch_d<112>(a, s, stream);
+  else launch_d<128>(a, s, stream);
+  return hipGetLastError();
+}
+
+}  // namespace sva

@@ -115,7 +115,16 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
   for (int e = threadIdx.x; e < nt * np; e += kThreads) {
     const int tk = e / np, p = e - tk * np;
     const int b = (t0 + tk) / a.N, n = t0 + tk - b * a.N;
-    double turn = (double)a.pos[b * a.pos_b + n] * (a.freq[p] * 0.15915494309189533576888);   // 1 / 2pi
+    double at;
+    if (!a.axis) {
+      at = (double)a.pos[b * a.pos_b + n];
+    } else {
+      // a pair of no axis stays where it is
+      const unsigned axis = a.axis[p];
+      const int64_t i = b * a.pos_b + n * a.pos_n + axis * a.pos_a;
+      at = axis >= (unsigned)a.axes ? 0.0 : a.pos_f32 ? (double)reinterpret_cast<const float*>(a.pos)[i] : (double)a.pos[i];
+    }
+    double turn = at * (a.freq[p] * 0.15915494309189533576888);   // 1 / 2pi
     turn -= rint(turn);
     float sn, cs;
     sincospif(2.0f * (float)turn, &sn, &cs);

@@ -9,77 +9,13 @@
 #include <algorithm>
 
 #include "../../include/sva.h"
+#include "api_checks.h"
 #include "sva_internal.h"
 
 namespace {
 
 using sva::HeadsView;
-
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) % n) == 0; }
-
-int hip_status(hipError_t e) { return e == hipSuccess ? SVA_OK : SVA_ERR_HIP; }
-
-// One strided tensor [B, heads, N, D]: its view, and the bytes from its first
-// element to behind its last.
-struct Tensor {
-  HeadsView v;
-  size_t span;
-  int align;                     // what data and strides are multiples of: 16, 8, 4 or 2 bytes
-};
-
-int check_heads(const sva_heads* h, int64_t B, int64_t N, int64_t D, size_t item, bool wide, bool output, Tensor* t) {
-  if (!h || !h->data || h->heads < 1) return SVA_ERR_INVALID_ARG;
-  if (h->stride_b < 0 || h->stride_h < 0 || h->stride_n < 0) return SVA_ERR_INVALID_ARG;
-  struct Dim {
-    int64_t size, stride;
-  };
-  // a dimension of one has no stride
-  Dim dims[3] = {{B, B > 1 ? h->stride_b : 0}, {h->heads, h->heads > 1 ? h->stride_h : 0}, {N, N > 1 ? h->stride_n : 0}};
-  int64_t span = D;
-  for (const Dim& d : dims) {
-    int64_t x;
-    if (__builtin_mul_overflow(d.size - 1, d.stride, &x) || __builtin_add_overflow(span, x, &span)) return SVA_ERR_SHAPE;
-  }
-  if (span > ((int64_t)1 << 58)) return SVA_ERR_SHAPE;
-  int align = 16;
-  auto fits = [&](int n) {
-    bool all = aligned(h->data, n);
-    for (const Dim& d : dims) all = all && d.stride * (int64_t)item % n == 0;
-    return all;
-  };
-  while (align > (int)item && !fits(align)) align /= 2;
-  if (!aligned(h->data, item) || (wide && align < 16)) return SVA_ERR_ALIGNMENT;
-  if (output) {                  // rows must not overlap
-    std::sort(dims, dims + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
-    int64_t reach = D;
-    for (const Dim& d : dims) {
-      if (d.size == 1) continue;
-      if (d.stride < reach) return SVA_ERR_INVALID_ARG;
-      reach += (d.size - 1) * d.stride;
-    }
-  }
-  t->v.p = h->data;
-  t->v.sb = h->stride_b;
-  t->v.sh = h->stride_h;
-  t->v.sn = h->stride_n;
-  t->v.heads = h->heads;
-  t->span = (size_t)span * item;
-  t->align = align;
-  return SVA_OK;
-}
-
-bool apart(const Tensor& x, const Tensor& y) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(x.v.p), b = reinterpret_cast<uintptr_t>(y.v.p);
-  return a + x.span <= b || b + y.span <= a;
-}
-
-bool same(const Tensor& x, const Tensor& y, int64_t B, int64_t N) {
-  return x.v.p == y.v.p && (B == 1 || x.v.sb == y.v.sb) && (x.v.heads == 1 || x.v.sh == y.v.sh) &&
-         (N == 1 || x.v.sn == y.v.sn);
-}
-
-bool good_dtype(int32_t t) { return t == SVA_BF16 || t == SVA_F32; }
-size_t item_of(int32_t t) { return t == SVA_F32 ? 4 : 2; }
+using namespace sva::api;
 
 int check_cache(const sva_cache* c, bool pointers, sva::CacheView* out) {
   if (!c) return SVA_ERR_INVALID_ARG;
@@ -163,6 +99,61 @@ int check_query(const sva_cache* cache, bool pointers, const sva_cache_query* q,
   return SVA_OK;
 }
 
+// `a` has the positions
+int rotary(const sva_rotary_params* p, const double* freq, const sva_heads* q_in, const sva_heads* q_out,
+           const sva_heads* k_in, const sva_heads* k_out, sva::RotaryArgs a, void* stream) {
+  if (p->batch < 1 || p->tokens < 1 || p->head_dim < 2 || p->rot_dim < 2 || p->rot_dim % 2 != 0 ||
+      p->rot_dim > p->head_dim)
+    return SVA_ERR_INVALID_ARG;
+  if (p->layout != SVA_ROTARY_HALF && p->layout != SVA_ROTARY_INTERLEAVED) return SVA_ERR_INVALID_ARG;
+  if (!good_dtype(p->dtype) || !isfinite(p->magnitude) || a.pos_b < 0) return SVA_ERR_INVALID_ARG;
+  if (p->head_dim > 1024 || p->rot_dim > 512) return SVA_ERR_UNSUPPORTED;
+  const int64_t B = p->batch, N = p->tokens, D = p->head_dim;
+  if (B * N > INT32_MAX || (B > 1 && a.pos_b > (int64_t)1 << 40)) return SVA_ERR_SHAPE;
+  if (!aligned(freq, 8) || !aligned(a.pos, 4)) return SVA_ERR_ALIGNMENT;
+  const size_t item = item_of(p->dtype);
+  Tensor qi, qo, ki{}, ko{};
+  int st;
+  if ((st = check_heads(q_in, B, N, D, item, false, false, &qi)) != SVA_OK) return st;
+  if ((st = check_heads(q_out, B, N, D, item, false, true, &qo)) != SVA_OK) return st;
+  if (qi.v.heads != qo.v.heads) return SVA_ERR_SHAPE;
+  const bool q_place = same(qi, qo, B, N);
+  if (!q_place && !apart(qi, qo)) return SVA_ERR_INVALID_ARG;
+  int piece = std::min(qi.align, qo.align);
+  bool k_place = true;
+  if (k_in) {
+    if ((st = check_heads(k_in, B, N, D, item, false, false, &ki)) != SVA_OK) return st;
+    if ((st = check_heads(k_out, B, N, D, item, false, true, &ko)) != SVA_OK) return st;
+    if (ki.v.heads != ko.v.heads) return SVA_ERR_SHAPE;
+    k_place = same(ki, ko, B, N);
+    if (!k_place && !apart(ki, ko)) return SVA_ERR_INVALID_ARG;
+    if (qo.v.p == ko.v.p || qo.v.p == ki.v.p || ko.v.p == qi.v.p) return SVA_ERR_INVALID_ARG;
+    piece = std::min({piece, ki.align, ko.align});
+  }
+  if ((int64_t)qi.v.heads + ki.v.heads > 1 << 20) return SVA_ERR_SHAPE;
+  a.qi = qi.v;
+  a.qo = qo.v;
+  a.ki = ki.v;
+  a.ko = ko.v;
+  a.freq = freq;
+  a.B = p->batch;
+  a.N = p->tokens;
+  a.D = p->head_dim;
+  a.rot = p->rot_dim;
+  a.magnitude = (float)p->magnitude;
+  a.f32 = p->dtype == SVA_F32;
+  a.half = p->layout == SVA_ROTARY_HALF;
+  a.backward = p->backward != 0;
+  a.copy = !(q_place && k_place);
+  // bytes of an access: a whole number of them makes the turned part (each half of it) and the rest
+  const int64_t turned = (int64_t)p->rot_dim * item / (a.half ? 2 : 1), row = a.copy ? D * (int64_t)item : 0;
+  while (piece > (int)item && (turned % piece != 0 || row % piece != 0)) piece /= 2;
+  a.piece = piece;
+  const int64_t rest = a.copy ? (D - p->rot_dim) * (int64_t)item : 0;
+  a.ragged = piece >= 4 && turned >= 16 && (rest == 0 || rest >= 16);
+  return hip_status(sva::launch_rotary(a, static_cast<hipStream_t>(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -199,59 +190,54 @@ int sva_rotary(const sva_rotary_params* p, const double* freq, const int32_t* po
                const sva_heads* q_in, const sva_heads* q_out, const sva_heads* k_in, const sva_heads* k_out,
                void* stream) {
   if (!p || !freq || !positions || !q_in || !q_out || (!k_in) != (!k_out)) return SVA_ERR_INVALID_ARG;
-  if (p->batch < 1 || p->tokens < 1 || p->head_dim < 2 || p->rot_dim < 2 || p->rot_dim % 2 != 0 ||
-      p->rot_dim > p->head_dim)
-    return SVA_ERR_INVALID_ARG;
-  if (p->layout != SVA_ROTARY_HALF && p->layout != SVA_ROTARY_INTERLEAVED) return SVA_ERR_INVALID_ARG;
-  if (!good_dtype(p->dtype) || !isfinite(p->magnitude) || pos_stride_b < 0) return SVA_ERR_INVALID_ARG;
-  if (p->head_dim > 1024 || p->rot_dim > 512) return SVA_ERR_UNSUPPORTED;
-  const int64_t B = p->batch, N = p->tokens, D = p->head_dim;
-  if (B * N > INT32_MAX || (B > 1 && pos_stride_b > (int64_t)1 << 40)) return SVA_ERR_SHAPE;
-  if (!aligned(freq, 8) || !aligned(positions, 4)) return SVA_ERR_ALIGNMENT;
-  const size_t item = item_of(p->dtype);
-  Tensor qi, qo, ki{}, ko{};
-  int st;
-  if ((st = check_heads(q_in, B, N, D, item, false, false, &qi)) != SVA_OK) return st;
-  if ((st = check_heads(q_out, B, N, D, item, false, true, &qo)) != SVA_OK) return st;
-  if (qi.v.heads != qo.v.heads) return SVA_ERR_SHAPE;
-  const bool q_place = same(qi, qo, B, N);
-  if (!q_place && !apart(qi, qo)) return SVA_ERR_INVALID_ARG;
-  int piece = std::min(qi.align, qo.align);
-  bool k_place = true;
-  if (k_in) {
-    if ((st = check_heads(k_in, B, N, D, item, false, false, &ki)) != SVA_OK) return st;
-    if ((st = check_heads(k_out, B, N, D, item, false, true, &ko)) != SVA_OK) return st;
-    if (ki.v.heads != ko.v.heads) return SVA_ERR_SHAPE;
-    k_place = same(ki, ko, B, N);
-    if (!k_place && !apart(ki, ko)) return SVA_ERR_INVALID_ARG;
-    if (qo.v.p == ko.v.p || qo.v.p == ki.v.p || ko.v.p == qi.v.p) return SVA_ERR_INVALID_ARG;
-    piece = std::min({piece, ki.align, ko.align});
-  }
-  if ((int64_t)qi.v.heads + ki.v.heads > 1 << 20) return SVA_ERR_SHAPE;
   sva::RotaryArgs a{};
-  a.qi = qi.v;
-  a.qo = qo.v;
-  a.ki = ki.v;
-  a.ko = ko.v;
-  a.freq = freq;
   a.pos = positions;
   a.pos_b = pos_stride_b;
-  a.B = p->batch;
-  a.N = p->tokens;
-  a.D = p->head_dim;
-  a.rot = p->rot_dim;
-  a.magnitude = (float)p->magnitude;
-  a.f32 = p->dtype == SVA_F32;
-  a.half = p->layout == SVA_ROTARY_HALF;
-  a.backward = p->backward != 0;
-  a.copy = !(q_place && k_place);
-  // bytes of an access: a whole number of them makes the turned part (each half of it) and the rest
-  const int64_t turned = (int64_t)p->rot_dim * item / (a.half ? 2 : 1), row = a.copy ? D * (int64_t)item : 0;
-  while (piece > (int)item && (turned % piece != 0 || row % piece != 0)) piece /= 2;
-  a.piece = piece;
-  const int64_t rest = a.copy ? (D - p->rot_dim) * (int64_t)item : 0;
-  a.ragged = piece >= 4 && turned >= 16 && (rest == 0 || rest >= 16);
-  return hip_status(sva::launch_rotary(a, static_cast<hipStream_t>(stream)));
+  return rotary(p, freq, q_in, q_out, k_in, k_out, a, stream);
+}
+
+int sva_rotary_axes_frequencies(const sva_rotary_spec* axes, int32_t count, double* freq, int32_t* axis,
+                                double* magnitude) {
+  if (!axes || !freq || !axis || !magnitude || count < 1) return SVA_ERR_INVALID_ARG;
+  if (count > SVA_ROTARY_MAX_AXES) return SVA_ERR_UNSUPPORTED;
+  int pairs = 0;
+  for (int i = 0; i < count; ++i) {
+    if (axes[i].rot_dim < 2 || axes[i].rot_dim > 512) return SVA_ERR_INVALID_ARG;
+    pairs += axes[i].rot_dim / 2;
+  }
+  if (pairs > 256) return SVA_ERR_UNSUPPORTED;
+  int at = 0;
+  double m0 = 0.0;
+  for (int i = 0; i < count; ++i) {
+    double m;
+    const int st = sva_rotary_frequencies(&axes[i], freq + at, &m);
+    if (st != SVA_OK) return st;
+    if (i == 0) m0 = m;
+    if (m != m0) return SVA_ERR_INVALID_ARG;      // one factor for the whole row
+    for (int j = 0; j < axes[i].rot_dim / 2; ++j) axis[at++] = i;
+  }
+  *magnitude = m0;
+  return SVA_OK;
+}
+
+int sva_rotary_axes(const sva_rotary_params* p, const double* freq, const int32_t* axis, const sva_positions* pos,
+                    const sva_heads* q_in, const sva_heads* q_out, const sva_heads* k_in, const sva_heads* k_out,
+                    void* stream) {
+  if (!p || !freq || !axis || !pos || !pos->data || !q_in || !q_out || (!k_in) != (!k_out)) return SVA_ERR_INVALID_ARG;
+  if (pos->axes < 1 || pos->stride_n < 0 || pos->stride_a < 0) return SVA_ERR_INVALID_ARG;
+  if (pos->type != SVA_POSITIONS_I32 && pos->type != SVA_POSITIONS_F32) return SVA_ERR_INVALID_ARG;
+  if (pos->axes > SVA_ROTARY_MAX_AXES) return SVA_ERR_UNSUPPORTED;
+  if (pos->stride_n > (int64_t)1 << 30 || pos->stride_a > (int64_t)1 << 31) return SVA_ERR_SHAPE;
+  if (!aligned(axis, 4)) return SVA_ERR_ALIGNMENT;
+  sva::RotaryArgs a{};
+  a.pos = static_cast<const int32_t*>(pos->data);
+  a.pos_b = pos->stride_b;
+  a.pos_n = pos->stride_n;
+  a.pos_a = pos->stride_a;
+  a.axis = axis;
+  a.axes = pos->axes;
+  a.pos_f32 = pos->type == SVA_POSITIONS_F32;
+  return rotary(p, freq, q_in, q_out, k_in, k_out, a, stream);
 }
 
 int sva_cache_write(const sva_cache* cache, int32_t batch, int32_t tokens, int32_t dtype, const sva_heads* k,
