@@ -691,8 +691,8 @@ typedef struct sva_cross {
                             float32 (c, c * log2(e)) is refused                     */
 } sva_cross;
 
-/* Bytes of device workspace of the two calls below (masked: with a mask): lists of keys,
- * and partial results where few rows meet many keys (or few keys many rows).  Host
+/* Bytes of device workspace of the two calls below (masked: with a mask): its bits, and
+ * partial results where few rows meet many keys (or few keys many rows).  Host
  * only. */
 int sva_cross_attention_workspace(const sva_cross* p, int32_t masked, size_t* bytes);
 int sva_cross_attention_backward_workspace(const sva_cross* p, int32_t masked, size_t* bytes);

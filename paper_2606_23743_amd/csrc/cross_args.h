@@ -16,8 +16,8 @@ struct CrossArgs {
   const int32_t* lens;           // [B] keys of an entry, null: M
   const uint8_t* mask;           // [B, M], null: none
   int64_t mask_b;
-  int32_t* rows;                 // with a mask: [B, M], the seen keys in order, then the hidden ones
-  int32_t* seen;                 // with a mask: [B], how many are seen
+  uint32_t* bits;                // with a mask: [B, ceil(M / 32)], bit j of word i: key 32i + j is seen
+  int32_t* seen;                 // with a mask: [B], keys up to the last seen one
   float* lse;                    // [B, H, N]; forward: written where not null; backward: read
   float* part;                   // partial results where keys (backward: or rows) are divided
   float* part_kv;                // backward: partial dK and dV
@@ -27,6 +27,7 @@ struct CrossArgs {
   float scale, scale_log2;
   int D;
   int tiles, splits;             // row tiles of a kv head; parts its keys are divided into
+  int run;                       // row tiles that a workgroup takes one after the other (one where keys are divided)
   int key_tiles, row_splits;     // backward: 128-key tiles, parts the rows are divided into
   int wgs, kv_wgs;               // workgroups of the launches
 };
@@ -34,13 +35,13 @@ struct CrossArgs {
 // How a call is divided, and its workspace: offsets of what CrossArgs points to.
 struct CrossShape {
   int narrow;                    // 16 rows a wave (64 a workgroup), else 32 (128)
-  int tiles, splits, key_tiles, row_splits;
-  size_t rows_at, seen_at, stat_at, stat_l_at, part_at, part_kv_at, ws_bytes;
+  int run, tiles, splits, key_tiles, row_splits;
+  size_t bits_at, seen_at, stat_at, stat_l_at, part_at, part_kv_at, ws_bytes;
 };
 CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask);
 CrossShape cross_grad_shape(int B, int Hkv, int G, int N, int M, int D, bool mask);
 
-hipError_t launch_cross_rows(const CrossArgs& a, hipStream_t stream);
+hipError_t launch_cross_bits(const CrossArgs& a, hipStream_t stream);
 hipError_t launch_cross_attention(const CrossArgs& a, const CrossShape& s, hipStream_t stream);
 hipError_t launch_cross_attention_grad(const CrossArgs& a, const CrossShape& s, hipStream_t stream);
 

@@ -10,8 +10,8 @@
 // passes it by 2^30, so weights, their sum and O stay far inside float32 while O is
 // almost never rescaled.  O is divided by the sum of the weights as they were rounded
 // to bf16 for the product, the log-sum-exp is that of the unrounded ones.
-// Hidden keys are not loaded at all: a length ends the walk, a mask is first turned
-// into the list of the keys it leaves.  Where few rows meet many keys, the keys are
+// Hidden keys are not loaded at all: a length ends the walk, as a mask's last seen key
+// does, and in place of those a mask hides before it zeros are loaded.  Where few rows meet many keys, the keys are
 // divided among workgroups and their results joined by a second launch.
 #include "cross_tiles.h"
 
@@ -25,73 +25,48 @@ constexpr int NST = 4, PD = 3;   // LDS stages, tiles ahead
 // a row's reference moves when a logit passes it by this much (log2 units)
 constexpr float kSlack = 30.0f;
 
-template <int D, int QT, bool GATHER, bool LSE>
+template <int D, int QT, bool MASK, bool LSE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, QT == 2 ? 2 : 4)))
 void cross_attn_kernel(CrossArgs a) {
   using G16 = Geo16<D>;
-  using Loader = TileLoader<D>;
-  constexpr int CT = Loader::CT, NUW = Loader::NUW;
+  using Feed = KeyFeed<D, MASK>;
+  constexpr int CT = TileLoader<D>::CT;
   __shared__ __attribute__((aligned(1024))) unsigned char Ks[NST][CT];
   __shared__ __attribute__((aligned(1024))) unsigned char Vs[NST][CT];
-  __shared__ int ring[GATHER ? RowRing::kSize : 1];
 
-  const int lane = threadIdx.x & 63, i = lane & 15;
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // (kv head of an entry, part of its keys, row tile)
-  const int id = __builtin_amdgcn_readfirstlane(xcd_remap(blockIdx.x, a.wgs));
-  const int per = a.tiles * a.splits, bh = id / per, rest = id - bh * per;
-  const int split = rest / a.tiles, tile = rest - split * a.tiles;
-  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
-
-  // this part's keys
-  const int count = seen_keys_of_all(a, b);
-  const int chunks_all = (count + CK - 1) / CK;
-  const int c0 = (int)((int64_t)chunks_all * split / a.splits), c1 = (int)((int64_t)chunks_all * (split + 1) / a.splits);
-  const int chunks = c1 - c0;
-
-  const int row0 = tile * 64 * QT + w * 16 * QT;
-  const uint16_t* Kh = static_cast<const uint16_t*>(a.k.p) + b * a.k.sb + kvh * a.k.sh;
-  const uint16_t* Vh = static_cast<const uint16_t*>(a.v.p) + b * a.v.sb + kvh * a.v.sh;
   const float sl2 = a.scale_log2;
-
-  Loader ld;
-  ld.init(w, lane);
   const unsigned ks_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Ks[0][0]);
   const unsigned vs_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Vs[0][0]);
-  RowRing rr{ring, GATHER ? a.rows + (int64_t)b * a.M : nullptr, count};
-  // tile c0 + c into stage st; one past the part's end loads zeros, so that every step waits for as many
-  auto fetch = [&](int st, int c) {
-    const int first = (c0 + c) * CK, end = c < chunks ? count : 0;
-    if constexpr (GATHER) {
-      int list[NUW];
-#pragma unroll
-      for (int u = 0; u < NUW; ++u) list[u] = c < chunks ? rr.at(first + ld.row[u]) : 0;
-      ld.load_rows(Kh, a.k.sn, list, end - first, ks_base + st * CT);
-      ld.load_rows(Vh, a.v.sn, list, end - first, vs_base + st * CT);
-    } else {
-      ld.load(Kh, a.k.sn, first, end, ks_base + st * CT);
-      ld.load(Vh, a.v.sn, first, end, vs_base + st * CT);
-    }
-  };
 
-  bf16x8 qop[QT][G16::KS];
-  const uint16_t* qrow[QT];
+  const Item it(a);
+  const int64_t bh = (int64_t)it.b * a.Hkv + it.kvh;
+  auto row_of = [&](int tile, int qt) { return tile * 64 * QT + (w * QT + qt) * 16 + i; };
+  auto load_q = [&](bf16x8 (&op)[QT][G16::KS], int tile) {
+    const uint16_t* rows[QT];
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const int r = row0 + qt * 16 + i;
-    qrow[qt] = r < a.R ? static_cast<const uint16_t*>(a.q.p) + row_offset(a.q, b, kvh * a.G, r, a.N) : nullptr;
-  }
-  load_operand<D>(qop, qrow, lane);
+    for (int qt = 0; qt < QT; ++qt) {
+      const int r = row_of(tile, qt);
+      rows[qt] = r < a.R ? static_cast<const uint16_t*>(a.q.p) + row_offset(a.q, it.b, it.kvh * a.G, r, a.N, a.G) : nullptr;
+    }
+    load_operand<D>(op, rows, lane);
+  };
 
   int koff[G16::KS], voff[G16::DT];
   operand_offsets<D>(lane, koff, voff);
-  float m_ref[QT], l_part[QT] = {}, l_full[QT] = {}, limit[QT];
-  f32x4 oacc[G16::DT][QT] = {};
+  float m_ref[QT], l_part[QT], l_full[QT], limit[QT];
+  f32x4 oacc[G16::DT][QT];
+  auto clear = [&]() {
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    m_ref[qt] = -3e38f;
-    limit[qt] = -INFINITY;
-  }
+    for (int qt = 0; qt < QT; ++qt) {
+      m_ref[qt] = -3e38f;
+      limit[qt] = -INFINITY;
+      l_part[qt] = l_full[qt] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < G16::DT; ++dt) oacc[dt][qt] = f32x4{};
+    }
+  };
 
   // moves the reference of rows that have a logit above their limit
   auto follow = [&](const f32x4 (&s)[2][QT]) {
@@ -145,86 +120,113 @@ void cross_attn_kernel(CrossArgs a) {
       if constexpr (LSE) l_full[qt] = lf;
     }
   };
-
-  if (chunks > 0) {
-    if constexpr (GATHER) {
-      rr.fill(c0 * CK);
-      rr.fill(c0 * CK + RowRing::kHalf);
-      __syncthreads();
-    }
+  auto store = [&](int tile) {
 #pragma unroll
-    for (int c = 0; c < PD; ++c) fetch(c, c);
-    // Tile c's loads are 2 * NUW of this wave's; Q's came before them.
-    wait_vmcnt<2 * NUW * (PD - 1)>();
-    wg_barrier();
-    f32x4 sacc[2][QT];
-    qk16<D>(sacc, &Ks[0][0], koff, qop);
-    if (count - c0 * CK < CK) mask_tail16(sacc, count - c0 * CK, lane);
-    int st = 0;
+    for (int qt = 0; qt < QT; ++qt) {
+      const float l_tot = quad_sum(l_part[qt]);
+      const float l_all = LSE ? quad_sum(l_full[qt]) : l_tot;
+      const int r = row_of(tile, qt);
+      const bool there = r < a.R;
+      if (a.splits > 1) {
+        if (!there) continue;
+        const int64_t at = (bh * a.splits + it.split) * a.R + r;
+        float* o = a.part + at * D;
+#pragma unroll
+        for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = oacc[dt][qt];
+        if (g == 0) {
+          a.stat[at] = make_float2(m_ref[qt], l_tot);
+          if constexpr (LSE) a.stat_l[at] = l_all;
+        }
+        continue;
+      }
+      const bool has = l_tot > 0.0f || l_tot != l_tot;   // a NaN stays one
+      uint16_t* o = there ? static_cast<uint16_t*>(a.out.p) + row_offset(a.out, it.b, it.kvh * a.G, r, a.N, a.G) : nullptr;
+      store_row<D>(o, &oacc[0][qt], QT, has ? 1.0f / l_tot : 0.0f, g);
+      if constexpr (LSE) {
+        if (g == 0 && there) a.lse[bh * a.R + r] = has ? (m_ref[qt] + __log2f(l_all)) * 0.69314718055994530942f : -INFINITY;
+      }
+    }
+  };
+
+  clear();
+  if (it.chunks == 0) {            // no key: zeros
+    for (int t = 0; t < it.tiles; ++t) store(it.tile + t);
+    return;
+  }
+  Feed feed;
+  feed.start(a, it, w, lane);
+  feed.ld.clear_pads(&Ks[0][0], NST);
+  feed.ld.clear_pads(&Vs[0][0], NST);
+  auto fetch = [&](int st) { return feed.feed(a, ks_base + st * CT, vs_base + st * CT); };
+  bf16x8 qop[QT][G16::KS], qnext[QT][G16::KS];
+  load_q(qop, it.tile);
+  // keys seen of the tiles ahead
+  uint32_t seen[PD];
+#pragma unroll
+  for (int c = 0; c < PD; ++c) seen[c] = fetch(c);
+  wait_vmcnt_lds_idle<Feed::kLoads * (PD - 1)>();      // tile 0 has landed, Q before it
+  wg_barrier();
+  f32x4 sacc[2][QT];
+  qk16<D>(sacc, &Ks[0][0], koff, qop);
+  if (seen[0] != ~0u) hide(sacc, seen[0], lane);
+
+  // A step is one tile of keys, in stage st: its softmax and product with V, and S of the
+  // tile after it, which past the last is the first one again for the next row tile.
+  int st = 0, c = 0, late = 0, tile = it.tile;
+  const int end = it.tile + it.tiles, ahead = max(it.chunks - 4, 0);
+  bool pending = false;            // a row tile whose result is not stored yet
 #pragma unroll 1
-    for (int c = 0; c < chunks; ++c) {
-      wait_vmcnt_lds_idle<2 * NUW * (PD - 2)>();     // tile c + 1 has landed
-      wg_barrier();                                  // and every wave is done with tile c - 1
-      if constexpr (GATHER) {
-        if (c != 0 && c % (RowRing::kHalf / CK) == 0) rr.fill(c0 * CK + c * CK + RowRing::kHalf);
-      }
-      fetch((st + PD) % NST, c + PD);
-      follow(sacc);
-      f32x4 snext[2][QT];
-      bf16x8 pop[QT];
-      qk16<D>(snext, &Ks[0][0] + (st + 1) % NST * CT, koff, qop);
-      softmax(sacc, pop);
-      __builtin_amdgcn_s_setprio(1);
-      pv16<D>(pop, &Vs[0][0] + st * CT, voff, oacc);
-      __builtin_amdgcn_s_setprio(0);
-      const int left = __builtin_amdgcn_readfirstlane(count - (c0 + c + 1) * CK);
-      if (__builtin_expect(left < CK, 0)) {
-        asm volatile("");
-        mask_tail16(snext, left, lane);
-      }
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) sacc[x][qt] = snext[x][qt];
-      st = (st + 1) % NST;
+  while (true) {
+    // The next tile has landed; in the two steps after Q's loads those may still be under way.
+    if (late > 0) wait_vmcnt_lds_idle<Feed::kLoads * (PD - 2) + QT * G16::KS>();
+    else wait_vmcnt_lds_idle<Feed::kLoads * (PD - 2)>();
+    --late;
+    wg_barrier();                  // and every wave is done with the tile before
+    if (pending) {                 // (stored here, ahead of loads that are waited for two steps later)
+      store(tile - 1);
+      clear();
+      pending = false;
+      if (tile == end) break;
     }
-    wait_vmcnt<0>();               // no load may still target this workgroup's LDS
+    const uint32_t fed = fetch((st + PD) % NST);
+    if (c == ahead) {              // Q of the next row tile, four tiles of keys before it is used
+      asm volatile("" ::: "memory");     // behind the tile's loads: the next waits count on it
+      if (tile + 1 < end) {
+        load_q(qnext, tile + 1);
+        late = 2;
+      }
+    }
+    follow(sacc);
+    if (++c == it.chunks) {
+      c = 0;
+      ++tile;
+      pending = true;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int s = 0; s < G16::KS; ++s) qop[qt][s] = qnext[qt][s];
+    }
+    f32x4 snext[2][QT];
+    bf16x8 pop[QT];
+    qk16<D>(snext, &Ks[0][0] + (st + 1) % NST * CT, koff, qop);
+    softmax(sacc, pop);
+    __builtin_amdgcn_s_setprio(1);
+    pv16<D>(pop, &Vs[0][0] + st * CT, voff, oacc);
+    __builtin_amdgcn_s_setprio(0);
+    if (__builtin_expect(seen[1] != ~0u, 0)) {
+      asm volatile("");
+      hide(snext, seen[1], lane);
+    }
+#pragma unroll
+    for (int x = 1; x < PD; ++x) seen[x - 1] = seen[x];
+    seen[PD - 1] = fed;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) sacc[x][qt] = snext[x][qt];
+    st = (st + 1) % NST;
   }
-
-  const int g = lane >> 4;
-#pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const float l_tot = quad_sum(l_part[qt]);
-    const float l_all = LSE ? quad_sum(l_full[qt]) : l_tot;
-    const int r = row0 + qt * 16 + i;
-    if (r >= a.R) continue;
-    if (a.splits > 1) {
-      const int64_t at = ((int64_t)bh * a.splits + split) * a.R + r;
-      float* o = a.part + at * D;
-#pragma unroll
-      for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = oacc[dt][qt];
-      if (g == 0) {
-        a.stat[at] = make_float2(m_ref[qt], l_tot);
-        if constexpr (LSE) a.stat_l[at] = l_all;
-      }
-      continue;
-    }
-    const bool has = l_tot > 0.0f || l_tot != l_tot;   // a NaN stays one
-    const float inv = has ? 1.0f / l_tot : 0.0f;
-    uint16_t* o = static_cast<uint16_t*>(a.out.p) + row_offset(a.out, b, kvh * a.G, r, a.N);
-#pragma unroll
-    for (int dt = 0; dt < G16::DT; ++dt) {
-      const bf16x2 x = cvt2(oacc[dt][qt][0] * inv, oacc[dt][qt][1] * inv);
-      const bf16x2 y = cvt2(oacc[dt][qt][2] * inv, oacc[dt][qt][3] * inv);
-      const bf16x4 z = {x[0], x[1], y[0], y[1]};
-      *reinterpret_cast<bf16x4*>(o + dt * 16 + 4 * g) = z;
-    }
-    if constexpr (LSE) {
-      if (g == 0)
-        a.lse[((int64_t)b * a.H + kvh * a.G) * a.N + r] =
-            has ? (m_ref[qt] + __log2f(l_all)) * 0.69314718055994530942f : -INFINITY;
-    }
-  }
+  wait_vmcnt<0>();                 // no load may still target this workgroup's LDS
 }
 
 // Joins the parts of a row: O = sum of 2^(m_s - m) O_s over the same of l_s.  One
@@ -276,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
   const bool has = l > 0.0f || l != l;
   const float inv = has ? 1.0f / l : 0.0f;
   if (2 * lane < D) {
-    uint16_t* o = static_cast<uint16_t*>(a.out.p) + row_offset(a.out, b, kvh * a.G, r, a.N);
+    uint16_t* o = static_cast<uint16_t*>(a.out.p) + row_offset(a.out, b, kvh * a.G, r, a.N, a.G);
     *reinterpret_cast<bf16x2*>(o + 2 * lane) = cvt2(o0 * inv, o1 * inv);
   }
   if constexpr (LSE) {
@@ -285,64 +287,41 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
   }
 }
 
-// The list of an entry's keys: those that mask and length leave, in order, then the
-// others, in order.  One workgroup an entry, 16 keys a lane at a time.
-constexpr int kListThreads = 1024, kListKeys = 16;
-__global__ __launch_bounds__(kListThreads) void cross_rows_kernel(CrossArgs a) {
+// An entry's mask and length as bits, a word for each tile of 32 keys, and its keys up to
+// the last seen one.  One workgroup an entry, a word a lane at a time.
+constexpr int kBitThreads = 1024;
+__global__ __launch_bounds__(kBitThreads) void cross_bits_kernel(CrossArgs a) {
   typedef unsigned __attribute__((ext_vector_type(4), aligned(1))) mask16;
-  __shared__ int sums[16];
-  const int b = blockIdx.x, M = a.M, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  __shared__ int last[kBitThreads / 64];
+  const int b = blockIdx.x, M = a.M, words = (M + 31) / 32;
   const uint8_t* mask = a.mask + b * a.mask_b;
   const int len = a.lens ? min(max(a.lens[b], 0), M) : M;
-  constexpr int kStep = kListThreads * kListKeys;
-  auto bits_at = [&](int key) -> unsigned {      // which of 16 keys are seen
-    unsigned bits = 0;
-    if (key + kListKeys <= M) {
-      const mask16 x = *reinterpret_cast<const mask16*>(mask + key);
+  uint32_t* bits = a.bits + (int64_t)b * words;
+  int end = 0;
+  for (int i = threadIdx.x; i < words; i += kBitThreads) {
+    const int key = i * 32;
+    uint32_t word = 0;
+    if (key + 32 <= M) {
 #pragma unroll
-      for (int e = 0; e < kListKeys; ++e) bits |= ((x[e / 4] >> (8 * (e % 4))) & 255u) != 0 ? 1u << e : 0u;
+      for (int h = 0; h < 2; ++h) {
+        const mask16 x = *reinterpret_cast<const mask16*>(mask + key + 16 * h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) word |= ((x[e / 4] >> (8 * (e % 4))) & 255u) != 0 ? 1u << (16 * h + e) : 0u;
+      }
     } else {
-      for (int e = 0; e < kListKeys; ++e)
-        if (key + e < M && mask[key + e]) bits |= 1u << e;
+      for (int e = 0; key + e < M; ++e) word |= mask[key + e] != 0 ? 1u << e : 0u;
     }
-    const int left = len - key;
-    return left >= kListKeys ? bits : left > 0 ? bits & ((1u << left) - 1u) : 0u;
-  };
-  // the sum over the workgroup of what each lane has, and what the lanes before it have
-  auto scan = [&](int x, int& before) -> int {
-    int run = x;
+    word &= rows_left(len - key);
+    bits[i] = word;
+    if (word) end = key + 32 - __clz(word);
+  }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(run, d);
-      if (lane >= d) run += y;
-    }
-    __syncthreads();
-    if (lane == 63) sums[w] = run;
-    __syncthreads();
-    int all = 0;
-    before = run - x;
-    for (int j = 0; j < kListThreads / 64; ++j) {
-      if (j < w) before += sums[j];
-      all += sums[j];
-    }
-    return all;
-  };
-  int mine = 0, before;
-  for (int key = threadIdx.x * kListKeys; key < M; key += kStep) mine += __popc(bits_at(key));
-  const int total = scan(mine, before);
-  if (threadIdx.x == 0) a.seen[b] = total;
-  int32_t* rows = a.rows + (int64_t)b * M;
-  int done = 0;                                   // seen keys of earlier steps
-  for (int first = 0; first < M; first += kStep) {
-    const int key = first + threadIdx.x * kListKeys;
-    const unsigned bits = key < M ? bits_at(key) : 0u;
-    const int all = scan(__popc(bits), before);
-    int seen = done + before, hidden = total + key - seen;
-    for (int e = 0; e < kListKeys && key + e < M; ++e) {
-      if (bits >> e & 1) rows[seen++] = key + e;
-      else rows[hidden++] = key + e;
-    }
-    done += all;
+  for (int d = 32; d > 0; d /= 2) end = max(end, __shfl_xor(end, d));
+  if (threadIdx.x % 64 == 0) last[threadIdx.x / 64] = end;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int j = 1; j < kBitThreads / 64; ++j) end = max(end, last[j]);
+    a.seen[b] = end;
   }
 }
 
@@ -371,17 +350,20 @@ static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask) {
   CrossShape s{};
   const int64_t heads = (int64_t)B * Hkv, R = (int64_t)G * N;
-  s.narrow = heads * ((R + 127) / 128) < 512;
+  const int64_t places = D == 64 ? 768 : 512;    // workgroups that the card holds: two a CU (D = 64: three)
+  s.narrow = heads * ((R + 127) / 128) < places;
   s.tiles = (int)((R + (s.narrow ? 63 : 127)) / (s.narrow ? 64 : 128));
   // keys are divided where the tiles are fewer than the card's places for workgroups
   const int64_t wgs = heads * s.tiles;
-  int64_t splits = wgs < 512 ? 1024 / wgs : 1;
+  int64_t splits = wgs < places ? places / wgs : 1;
   if (splits > (M + 255) / 256) splits = (M + 255) / 256;
   s.splits = (int)(splits < 1 ? 1 : splits);
+  const int64_t run = wgs / (4 * places);
+  s.run = (int)(run < 1 ? 1 : run < 8 ? run : 8);
   size_t at = 0;
   if (mask) {
-    s.rows_at = at;
-    at += up256((size_t)B * M * 4);
+    s.bits_at = at;
+    at += up256((size_t)B * ((M + 31) / 32) * 4);
     s.seen_at = at;
     at += up256((size_t)B * 4);
   }
@@ -398,14 +380,14 @@ CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask) {
   return s;
 }
 
-hipError_t launch_cross_rows(const CrossArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(cross_rows_kernel, dim3(a.B), dim3(kListThreads), 0, stream, a);
+hipError_t launch_cross_bits(const CrossArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(cross_bits_kernel, dim3(a.B), dim3(kBitThreads), 0, stream, a);
   return hipGetLastError();
 }
 
 hipError_t launch_cross_attention(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
   if (a.mask) {
-    const hipError_t e = launch_cross_rows(a, stream);
+    const hipError_t e = launch_cross_bits(a, stream);
     if (e != hipSuccess) return e;
   }
   if (a.D == 64) launch_d<64>(a, s, stream);

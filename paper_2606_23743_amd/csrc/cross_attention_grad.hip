@@ -24,68 +24,42 @@ using namespace cross;
 
 constexpr int NST = 4, PD = 3;   // LDS stages, tiles ahead
 
-template <int D, int QT, bool GATHER>
+template <int D, int QT, bool MASK>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, QT == 2 ? 2 : 4)))
 void cross_grad_rows_kernel(CrossArgs a) {
   using G16 = Geo16<D>;
-  using Loader = TileLoader<D>;
-  constexpr int CT = Loader::CT, NUW = Loader::NUW;
+  using Feed = KeyFeed<D, MASK>;
+  constexpr int CT = TileLoader<D>::CT;
   __shared__ __attribute__((aligned(1024))) unsigned char Ks[NST][CT];
   __shared__ __attribute__((aligned(1024))) unsigned char Vs[NST][CT];
-  __shared__ int ring[GATHER ? RowRing::kSize : 1];
 
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int id = __builtin_amdgcn_readfirstlane(xcd_remap(blockIdx.x, a.wgs));
-  const int per = a.tiles * a.splits, bh = id / per, rest = id - bh * per;
-  const int split = rest / a.tiles, tile = rest - split * a.tiles;
-  const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
-
-  const int count = seen_keys_of_all(a, b);
-  const int chunks_all = (count + CK - 1) / CK;
-  const int c0 = (int)((int64_t)chunks_all * split / a.splits), c1 = (int)((int64_t)chunks_all * (split + 1) / a.splits);
-  const int chunks = c1 - c0;
-
-  const int row0 = tile * 64 * QT + w * 16 * QT;
-  const uint16_t* Kh = static_cast<const uint16_t*>(a.k.p) + b * a.k.sb + kvh * a.k.sh;
-  const uint16_t* Vh = static_cast<const uint16_t*>(a.v.p) + b * a.v.sb + kvh * a.v.sh;
   const float sl2 = a.scale_log2;
-
-  Loader ld;
-  ld.init(w, lane);
   const unsigned ks_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Ks[0][0]);
   const unsigned vs_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Vs[0][0]);
-  RowRing rr{ring, GATHER ? a.rows + (int64_t)b * a.M : nullptr, count};
-  auto fetch = [&](int st, int c) {
-    const int first = (c0 + c) * CK, end = c < chunks ? count : 0;
-    if constexpr (GATHER) {
-      int list[NUW];
-#pragma unroll
-      for (int u = 0; u < NUW; ++u) list[u] = c < chunks ? rr.at(first + ld.row[u]) : 0;
-      ld.load_rows(Kh, a.k.sn, list, end - first, ks_base + st * CT);
-      ld.load_rows(Vh, a.v.sn, list, end - first, vs_base + st * CT);
-    } else {
-      ld.load(Kh, a.k.sn, first, end, ks_base + st * CT);
-      ld.load(Vh, a.v.sn, first, end, vs_base + st * CT);
-    }
-  };
+
+  const Item it(a);
+  const int64_t bh = (int64_t)it.b * a.Hkv + it.kvh;
+  auto row_of = [&](int tile, int qt) { return tile * 64 * QT + (w * QT + qt) * 16 + i; };
 
   // Q and dO of the wave's rows, their lse and delta
   bf16x8 qop[QT][G16::KS], gop[QT][G16::KS];
   float lse2[QT], delta[QT];
-  {
+  auto load_rows = [&](int tile) {
     const uint16_t *qrow[QT], *grow[QT], *orow[QT];
+    float lse[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-      const int r = row0 + qt * 16 + i;
-      const bool there = r < a.R;
-      const int rr_ = there ? r : 0;
-      qrow[qt] = there ? static_cast<const uint16_t*>(a.q.p) + row_offset(a.q, b, kvh * a.G, rr_, a.N) : nullptr;
-      grow[qt] = there ? static_cast<const uint16_t*>(a.dout.p) + row_offset(a.dout, b, kvh * a.G, rr_, a.N) : nullptr;
-      orow[qt] = there ? static_cast<const uint16_t*>(a.out.p) + row_offset(a.out, b, kvh * a.G, rr_, a.N) : nullptr;
-      // a row that saw no key has P = 0 everywhere
-      const float lse = there ? a.lse[(int64_t)bh * a.R + rr_] : -INFINITY;
-      lse2[qt] = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634074f;
+      const int r = row_of(tile, qt);
+      qrow[qt] = grow[qt] = orow[qt] = nullptr;
+      lse[qt] = -INFINITY;
+      if (r < a.R) {
+        qrow[qt] = static_cast<const uint16_t*>(a.q.p) + row_offset(a.q, it.b, it.kvh * a.G, r, a.N, a.G);
+        grow[qt] = static_cast<const uint16_t*>(a.dout.p) + row_offset(a.dout, it.b, it.kvh * a.G, r, a.N, a.G);
+        orow[qt] = static_cast<const uint16_t*>(a.out.p) + row_offset(a.out, it.b, it.kvh * a.G, r, a.N, a.G);
+        lse[qt] = a.lse[bh * a.R + r];
+      }
     }
     bf16x8 oop[QT][G16::KS];
     load_operand<D>(qop, qrow, lane);
@@ -99,83 +73,95 @@ void cross_grad_rows_kernel(CrossArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) s = fmaf((float)gop[qt][x][e], (float)oop[qt][x][e], s);
       delta[qt] = quad_sum(s);
-      const int r = row0 + qt * 16 + i;
-      if (split == 0 && g == 0 && r < a.R) a.stat[(int64_t)bh * a.R + r] = make_float2(lse2[qt], delta[qt]);
+      // a row that saw no key has P = 0 everywhere
+      lse2[qt] = lse[qt] == -INFINITY ? INFINITY : lse[qt] * 1.4426950408889634074f;
+      const int r = row_of(tile, qt);
+      if (it.split == 0 && g == 0 && r < a.R) a.stat[bh * a.R + r] = make_float2(lse2[qt], delta[qt]);
     }
+  };
+  f32x4 dq[G16::DT][QT] = {};
+  auto store = [&](int tile) {
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      const int r = row_of(tile, qt);
+      if (r < a.R && a.splits > 1) {
+        float* o = a.part + ((bh * a.splits + it.split) * a.R + r) * D;
+#pragma unroll
+        for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = dq[dt][qt];
+      } else if (a.splits == 1) {
+        uint16_t* o = r < a.R ? static_cast<uint16_t*>(a.dq.p) + row_offset(a.dq, it.b, it.kvh * a.G, r, a.N, a.G) : nullptr;
+        store_row<D>(o, &dq[0][qt], QT, a.scale, g);
+      }
+#pragma unroll
+      for (int dt = 0; dt < G16::DT; ++dt) dq[dt][qt] = f32x4{};
+    }
+  };
+
+  if (it.chunks == 0) {            // no key: zeros
+    for (int t = 0; t < it.tiles; ++t) {
+      load_rows(it.tile + t);
+      store(it.tile + t);
+    }
+    return;
   }
+  Feed feed;
+  feed.start(a, it, w, lane);
+  feed.ld.clear_pads(&Ks[0][0], NST);
+  feed.ld.clear_pads(&Vs[0][0], NST);
+  auto fetch = [&](int st) { return feed.feed(a, ks_base + st * CT, vs_base + st * CT); };
+  uint32_t seen[PD];               // which keys of the tiles ahead are
+#pragma unroll
+  for (int c = 0; c < PD; ++c) seen[c] = fetch(c);
+  load_rows(it.tile);
 
   int koff[G16::KS], voff[G16::DT];
   operand_offsets<D>(lane, koff, voff);
-  f32x4 dq[G16::DT][QT] = {};
-  if (chunks > 0) {
-    if constexpr (GATHER) {
-      rr.fill(c0 * CK);
-      rr.fill(c0 * CK + RowRing::kHalf);
-      __syncthreads();
-    }
-#pragma unroll
-    for (int c = 0; c < PD; ++c) fetch(c, c);
-    int st = 0;
+  int st = 0, c = 0, tile = it.tile;
+  const int end = it.tile + it.tiles;
 #pragma unroll 1
-    for (int c = 0; c < chunks; ++c) {
-      wait_vmcnt_lds_idle<2 * NUW * (PD - 1)>();     // tile c has landed
-      wg_barrier();                                  // and every wave is done with tile c - 1
-      if constexpr (GATHER) {
-        if (c != 0 && c % (RowRing::kHalf / CK) == 0) rr.fill(c0 * CK + c * CK + RowRing::kHalf);
-      }
-      fetch((st + PD) % NST, c + PD);
-      const unsigned char *kt = &Ks[0][0] + st * CT, *vt = &Vs[0][0] + st * CT;
-      f32x4 s[2][QT], dp[2][QT];
-      qk16<D>(s, kt, koff, qop);
-      qk16<D>(dp, vt, koff, gop);
-      const int left = __builtin_amdgcn_readfirstlane(count - (c0 + c) * CK);
-      if (__builtin_expect(left < CK, 0)) {
-        asm volatile("");
-        mask_tail16(s, left, lane);
-      }
-      bf16x8 dsop[QT];
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        u32x4 wv;
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e], sl2, -lse2[qt]));
-            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e + 1], sl2, -lse2[qt]));
-            const bf16x2 x = cvt2(p0 * (dp[k2][qt][2 * e] - delta[qt]), p1 * (dp[k2][qt][2 * e + 1] - delta[qt]));
-            wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, x);
-          }
-        dsop[qt] = __builtin_bit_cast(bf16x8, wv);
-      }
-      pv16<D>(dsop, kt, voff, dq);
-      st = (st + 1) % NST;
+  while (true) {
+    wait_vmcnt_lds_idle<Feed::kLoads * (PD - 1)>();    // the tile has landed
+    wg_barrier();                                      // and every wave is done with the one before
+    const uint32_t fed = fetch((st + PD) % NST);
+    const unsigned char *kt = &Ks[0][0] + st * CT, *vt = &Vs[0][0] + st * CT;
+    f32x4 s[2][QT], dp[2][QT];
+    qk16<D>(s, kt, koff, qop);
+    qk16<D>(dp, vt, koff, gop);
+    if (__builtin_expect(seen[0] != ~0u, 0)) {
+      asm volatile("");
+      hide(s, seen[0], lane);
     }
-    wait_vmcnt<0>();               // no load may still target this workgroup's LDS
-  }
-
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const int r = row0 + qt * 16 + i;
-    if (r >= a.R) continue;
-    if (a.splits > 1) {
-      float* o = a.part + (((int64_t)bh * a.splits + split) * a.R + r) * D;
+    for (int x = 1; x < PD; ++x) seen[x - 1] = seen[x];
+    seen[PD - 1] = fed;
+    bf16x8 dsop[QT];
 #pragma unroll
-      for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = dq[dt][qt];
-      continue;
+    for (int qt = 0; qt < QT; ++qt) {
+      u32x4 wv;
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e], sl2, -lse2[qt]));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e + 1], sl2, -lse2[qt]));
+          const bf16x2 x = cvt2(p0 * (dp[k2][qt][2 * e] - delta[qt]), p1 * (dp[k2][qt][2 * e + 1] - delta[qt]));
+          wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, x);
+        }
+      dsop[qt] = __builtin_bit_cast(bf16x8, wv);
     }
-    uint16_t* o = static_cast<uint16_t*>(a.dq.p) + row_offset(a.dq, b, kvh * a.G, r, a.N);
-#pragma unroll
-    for (int dt = 0; dt < G16::DT; ++dt) {
-      const bf16x2 x = cvt2(dq[dt][qt][0] * a.scale, dq[dt][qt][1] * a.scale);
-      const bf16x2 y = cvt2(dq[dt][qt][2] * a.scale, dq[dt][qt][3] * a.scale);
-      const bf16x4 z = {x[0], x[1], y[0], y[1]};
-      *reinterpret_cast<bf16x4*>(o + dt * 16 + 4 * g) = z;
+    pv16<D>(dsop, kt, voff, dq);
+    st = (st + 1) % NST;
+    if (++c == it.chunks) {
+      store(tile);
+      c = 0;
+      if (++tile == end) break;
+      load_rows(tile);
     }
   }
+  wait_vmcnt<0>();                 // no load may still target this workgroup's LDS
 }
 
-template <int D, bool GATHER>
+template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void cross_grad_keys_kernel(CrossArgs a) {
   using G16 = Geo16<D>;
@@ -188,14 +174,12 @@ void cross_grad_keys_kernel(CrossArgs a) {
 
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // (kv head of an entry, part of the rows, key tile)
-  const int id = __builtin_amdgcn_readfirstlane(xcd_remap(blockIdx.x, a.kv_wgs));
-  const int per = a.key_tiles * a.row_splits, bh = id / per, rest = id - bh * per;
-  const int split = rest / a.key_tiles, tile = rest - split * a.key_tiles;
+  // part of the rows, key tile, kv head of an entry (the fastest, as in the other kernels)
+  const int heads = a.B * a.Hkv, part = blockIdx.x / heads, bh = blockIdx.x - part * heads;
+  const int split = part / a.key_tiles, tile = part - split * a.key_tiles;
   const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
   const int count = seen_keys_of_all(a, b);
   const int key0 = tile * 128 + w * 32;
-  const int32_t* list = GATHER ? a.rows + (int64_t)b * a.M : nullptr;
   const float sl2 = a.scale_log2;
 
   f32x4 dk[G16::DT][KT] = {}, dv[G16::DT][KT] = {};
@@ -207,10 +191,9 @@ void cross_grad_keys_kernel(CrossArgs a) {
       for (int kt = 0; kt < KT; ++kt) {
         const int j = key0 + kt * 16 + i;
         krow[kt] = vrow[kt] = nullptr;
-        if (j < count) {
-          const int64_t key = GATHER ? list[j] : j;
-          krow[kt] = static_cast<const uint16_t*>(a.k.p) + b * a.k.sb + kvh * a.k.sh + key * a.k.sn;
-          vrow[kt] = static_cast<const uint16_t*>(a.v.p) + b * a.v.sb + kvh * a.v.sh + key * a.v.sn;
+        if (is_seen(a, b, j, count)) {
+          krow[kt] = static_cast<const uint16_t*>(a.k.p) + b * a.k.sb + kvh * a.k.sh + j * a.k.sn;
+          vrow[kt] = static_cast<const uint16_t*>(a.v.p) + b * a.v.sb + kvh * a.v.sh + j * a.v.sn;
         }
       }
       load_operand<D>(kop, krow, lane);
@@ -226,20 +209,37 @@ void cross_grad_keys_kernel(CrossArgs a) {
     const unsigned qs_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Qs[0][0]);
     const unsigned gs_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Gs[0][0]);
     const unsigned ss_base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)&Ss[0][0]);
+    ld.clear_pads(&Qs[0][0], NST);
+    ld.clear_pads(&Gs[0][0], NST);
     int64_t ft = t0;                             // the next tile to load
     int fh = (int)(t0 / per_head), fn = (int)(t0 - (int64_t)fh * per_head) * CK;
-    auto fetch = [&](int st) {
-      const int end = ft < t1 ? a.N : 0;
+    const uint16_t *qp, *gp;
+    const float2* sp;
+    auto bases = [&]() {
       const int64_t h = kvh * a.G + (ft < t1 ? fh : 0);
-      ld.load(static_cast<const uint16_t*>(a.q.p) + b * a.q.sb + h * a.q.sh, a.q.sn, fn, end, qs_base + st * CT);
-      ld.load(static_cast<const uint16_t*>(a.dout.p) + b * a.dout.sb + h * a.dout.sh, a.dout.sn, fn, end, gs_base + st * CT);
-      const float* from = reinterpret_cast<const float*>(a.stat + ((int64_t)b * a.H + h) * a.N + fn) + lane;
-      global_to_lds<4>(fn + lane / 2 < end ? from : kInf + (lane & 1), ss_base + st * (int)(CK * sizeof(float2)));
+      qp = static_cast<const uint16_t*>(a.q.p) + b * a.q.sb + h * a.q.sh + fn * a.q.sn;
+      gp = static_cast<const uint16_t*>(a.dout.p) + b * a.dout.sb + h * a.dout.sh + fn * a.dout.sn;
+      sp = a.stat + ((int64_t)b * a.H + h) * a.N + fn;
+    };
+    bases();
+    uint32_t qoff[NUW], goff[NUW];
+    ld.offsets(a.q.sn, qoff);
+    ld.offsets(a.dout.sn, goff);
+    auto fetch = [&](int st) {
+      const int left = ft < t1 ? a.N - fn : 0;
+      ld.load(qp, a.q.sn, qoff, rows_left(left), qs_base + st * CT);
+      ld.load(gp, a.dout.sn, goff, rows_left(left), gs_base + st * CT);
+      const float* from = reinterpret_cast<const float*>(sp) + lane;
+      global_to_lds<4>(lane / 2 < left ? from : kInf + (lane & 1), ss_base + st * (int)(CK * sizeof(float2)));
       ++ft;
       fn += CK;
+      qp += CK * a.q.sn;
+      gp += CK * a.dout.sn;
+      sp += CK;
       if (fn >= a.N) {
         fn = 0;
         ++fh;
+        bases();
       }
     };
     int koff[G16::KS], voff[G16::DT];
@@ -291,7 +291,6 @@ void cross_grad_keys_kernel(CrossArgs a) {
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int j = key0 + kt * 16 + i;
-    if (j >= a.M) continue;
     if (a.row_splits > 1) {
       if (j >= count) continue;                  // the join knows which are hidden
       float* k = a.part_kv + ((((int64_t)bh * a.row_splits + split) * 2) * a.M + j) * D;
@@ -303,20 +302,17 @@ void cross_grad_keys_kernel(CrossArgs a) {
       }
       continue;
     }
-    const bool there = j < count;
-    const int64_t key = GATHER ? list[j] : j;
-    uint16_t* k = static_cast<uint16_t*>(a.dk.p) + b * a.dk.sb + kvh * a.dk.sh + key * a.dk.sn;
-    uint16_t* v = static_cast<uint16_t*>(a.dv.p) + b * a.dv.sb + kvh * a.dv.sh + key * a.dv.sn;
+    if (!is_seen(a, b, j, count)) {              // a hidden key's gradients are zeros
 #pragma unroll
-    for (int dt = 0; dt < G16::DT; ++dt) {
-      const bf16x2 x = cvt2(dk[dt][kt][0] * a.scale, dk[dt][kt][1] * a.scale);
-      const bf16x2 y = cvt2(dk[dt][kt][2] * a.scale, dk[dt][kt][3] * a.scale);
-      const bf16x2 p = cvt2(dv[dt][kt][0], dv[dt][kt][1]), q = cvt2(dv[dt][kt][2], dv[dt][kt][3]);
-      const bf16x4 none = {};
-      const bf16x4 kz = {x[0], x[1], y[0], y[1]}, vz = {p[0], p[1], q[0], q[1]};
-      *reinterpret_cast<bf16x4*>(k + dt * 16 + 4 * g) = there ? kz : none;
-      *reinterpret_cast<bf16x4*>(v + dt * 16 + 4 * g) = there ? vz : none;
+      for (int dt = 0; dt < G16::DT; ++dt) dk[dt][kt] = dv[dt][kt] = f32x4{};
     }
+    uint16_t *k = nullptr, *v = nullptr;
+    if (j < a.M) {
+      k = static_cast<uint16_t*>(a.dk.p) + b * a.dk.sb + kvh * a.dk.sh + j * a.dk.sn;
+      v = static_cast<uint16_t*>(a.dv.p) + b * a.dv.sb + kvh * a.dv.sh + j * a.dv.sn;
+    }
+    store_row<D>(k, &dk[0][kt], KT, a.scale, g);
+    store_row<D>(v, &dv[0][kt], KT, 1.0f, g);
   }
 }
 
@@ -332,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossArgs a, int fi
   const int bh = (int)(at / rows), r = (int)(at - (int64_t)bh * rows);
   const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
   f32x4 s = {};
-  if (which == 0 || r < seen_keys(a, b)) {
+  if (which == 0 || is_seen(a, b, r, seen_keys(a, b))) {
     const float* from = which == 0 ? a.part + ((int64_t)bh * parts * rows + r) * D + c
                                    : a.part_kv + (((int64_t)bh * parts * 2 + (which - 1)) * rows + r) * D + c;
     const int64_t step = (int64_t)rows * D * (which == 0 ? 1 : 2);
@@ -344,8 +340,8 @@ __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossArgs a, int fi
   const bf16x4 z = {x[0], x[1], y[0], y[1]};
   int64_t off;
   const HeadsView& to = which == 0 ? a.dq : which == 1 ? a.dk : a.dv;
-  if (which == 0) off = row_offset(to, b, kvh * a.G, r, a.N);
-  else off = b * to.sb + kvh * to.sh + (int64_t)(a.mask ? a.rows[(int64_t)b * a.M + r] : r) * to.sn;
+  if (which == 0) off = row_offset(to, b, kvh * a.G, r, a.N, a.G);
+  else off = b * to.sb + kvh * to.sh + r * to.sn;
   *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(to.p) + off + c) = z;
 }
 
@@ -356,8 +352,7 @@ void launch_d(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
   else if (s.narrow) go(cross_grad_rows_kernel<D, 1, false>, a.wgs);
   else if (a.mask) go(cross_grad_rows_kernel<D, 2, true>, a.wgs);
   else go(cross_grad_rows_kernel<D, 2, false>, a.wgs);
-  if (a.mask) go(cross_grad_keys_kernel<D, true>, a.kv_wgs);
-  else go(cross_grad_keys_kernel<D, false>, a.kv_wgs);
+  go(cross_grad_keys_kernel<D>, a.kv_wgs);
   auto sum = [&](int first, int n, int64_t rows) {
     constexpr int kRows = kThreads / (D / 4);
     hipLaunchKernelGGL(cross_sum_kernel<D>, dim3((unsigned)((rows + kRows - 1) / kRows), n), dim3(kThreads), 0, stream, a, first);
@@ -391,7 +386,7 @@ CrossShape cross_grad_shape(int B, int Hkv, int G, int N, int M, int D, bool mas
 
 hipError_t launch_cross_attention_grad(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
   if (a.mask) {
-    const hipError_t e = launch_cross_rows(a, stream);
+    const hipError_t e = launch_cross_bits(a, stream);
     if (e != hipSuccess) return e;
   }
   if (a.D == 64) launch_d<64>(a, s, stream);

@@ -52,54 +52,77 @@ __device__ __forceinline__ void global_to_lds(const void* from, unsigned lds_add
 
 // Direct global -> LDS loads of one tile of 32 rows: the NUW 1 KB pieces a wave
 // fills.  Piece u covers tile rows u * RPI ..; lane L fills row u * RPI + L / NCH at
-// position L % NCH with the piece that the swizzle maps there.
+// position L % NCH with the piece that the swizzle maps there.  A pitch of D = 112 leaves
+// two positions of a row without a piece: those lanes load nothing, and what is there is
+// cleared once.
 template <int D>
 struct TileLoader {
   using G = Geo<D>;
   static constexpr int CT = CK * G::RB;          // bytes of a tile
   static constexpr int NUW = CT / 1024 / (kThreads / 64);
-  int row[NUW], chan[NUW];                       // of the tile, element offset in the row (negative: padding)
-  int w;
+  static constexpr bool PAD = G::DCH != G::NCH;
+  int w, lane;
 
-  __device__ __forceinline__ void init(int wave, int lane) {
+  __device__ __forceinline__ void init(int wave, int ln) {
     w = wave;
+    lane = ln;
+  }
+  __device__ __forceinline__ int row(int u) const { return (w * NUW + u) * G::RPI + lane / G::NCH; }
+  __device__ __forceinline__ int piece(int u) const { return swz<G::NCH>(row(u), lane % G::NCH); }
+  // zeros where no piece goes, in `stages` tiles from `tiles` on
+  __device__ __forceinline__ void clear_pads(unsigned char* tiles, int stages) const {
+    if constexpr (PAD) {
 #pragma unroll
-    for (int u = 0; u < NUW; ++u) {
-      row[u] = (wave * NUW + u) * G::RPI + lane / G::NCH;
-      const int c = swz<G::NCH>(row[u], lane % G::NCH);
-      chan[u] = c < G::DCH ? c * 8 : -1;
+      for (int u = 0; u < NUW; ++u)
+        if (piece(u) >= G::DCH)
+          for (int st = 0; st < stages; ++st) *reinterpret_cast<u32x4*>(tiles + st * CT + (w * NUW + u) * 1024 + lane * 16) = u32x4{};
     }
   }
-  // rows first .. first + 31 of `count` behind `base`, row pitch `pitch` elements
-  __device__ __forceinline__ void load(const uint16_t* base, int64_t pitch, int first, int count, unsigned lds) const {
-    if (__builtin_expect(first + CK <= count, 1) && G::DCH == G::NCH) {
-      const uint16_t* p = base + (int64_t)first * pitch;
+  // byte offsets of the lane's pieces from a tile's first row, where they fit in 32 bits
+  static __device__ __forceinline__ bool near(int64_t pitch) { return pitch < (int64_t)1 << 25; }
+  __device__ __forceinline__ void offsets(int64_t pitch, uint32_t (&off)[NUW]) const {
 #pragma unroll
-      for (int u = 0; u < NUW; ++u) global_to_lds<16>(p + (row[u] * pitch + chan[u]), lds + (w * NUW + u) * 1024);
-    } else {
+    for (int u = 0; u < NUW; ++u) off[u] = near(pitch) ? (uint32_t)(row(u) * (int)pitch + piece(u) * 8) * 2u : 0u;
+  }
+  // a whole tile whose first row is at `tile`
+  __device__ __forceinline__ void load_near(const uint16_t* tile, const uint32_t (&off)[NUW], unsigned lds) const {
 #pragma unroll
-      for (int u = 0; u < NUW; ++u) {
-        const bool there = first + row[u] < count && chan[u] >= 0;
-        const void* p = base + ((int64_t)first + row[u]) * pitch + chan[u];
-        global_to_lds<16>(there ? p : (const void*)kZeros, lds + (w * NUW + u) * 1024);
+    for (int u = 0; u < NUW; ++u)
+      if (!PAD || piece(u) < G::DCH)
+        global_to_lds<16>(reinterpret_cast<const unsigned char*>(tile) + off[u], lds + (w * NUW + u) * 1024);
+  }
+  // the rows of a tile whose bits are set, zeros in place of the others
+  __device__ __forceinline__ void load_some(const uint16_t* tile, int64_t pitch, uint32_t bits, unsigned lds) const {
+    // The lane id goes through an empty asm, so that what this rarer path needs is worked
+    // out here and not kept in registers.
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+#pragma unroll
+    for (int u = 0; u < NUW; ++u) {
+      const int r = (w * NUW + u) * G::RPI + ln / G::NCH, c = swz<G::NCH>(r, ln % G::NCH);
+      if (!PAD || c < G::DCH) {
+        const void* p = tile + (int64_t)r * pitch + c * 8;
+        global_to_lds<16>(bits >> r & 1 ? p : (const void*)kZeros, lds + (w * NUW + u) * 1024);
       }
     }
   }
-  // the rows that `list` (indexed by u) names, those from `valid` on being absent
-  __device__ __forceinline__ void load_rows(const uint16_t* base, int64_t pitch, const int (&list)[NUW], int valid, unsigned lds) const {
-#pragma unroll
-    for (int u = 0; u < NUW; ++u) {
-      const bool there = row[u] < valid && chan[u] >= 0;
-      const void* p = base + list[u] * pitch + chan[u];
-      global_to_lds<16>(there ? p : (const void*)kZeros, lds + (w * NUW + u) * 1024);
-    }
+  __device__ __forceinline__ void load(const uint16_t* tile, int64_t pitch, const uint32_t (&off)[NUW], uint32_t bits, unsigned lds) const {
+    if (__builtin_expect(bits == ~0u && near(pitch), 1)) load_near(tile, off, lds);
+    else load_some(tile, pitch, bits, lds);
   }
 };
 
-// keys of an entry that queries see
+// Which of a tile's 32 rows are there, `left` of them or more being left.
+__device__ __forceinline__ uint32_t rows_left(int left) { return left >= CK ? ~0u : left > 0 ? (1u << left) - 1u : 0u; }
+
+// keys of an entry up to the last that queries see
 __device__ __forceinline__ int seen_keys(const CrossArgs& a, int b) {
   const int n = a.mask ? a.seen[b] : a.lens ? a.lens[b] : a.M;
   return min(max(n, 0), a.M);
+}
+// whether queries see key m, one of the entry's `count` first
+__device__ __forceinline__ bool is_seen(const CrossArgs& a, int b, int m, int count) {
+  return m < count && (!a.mask || (a.bits[(int64_t)b * ((a.M + 31) / 32) + m / 32] >> (m % 32) & 1));
 }
 // the same of a workgroup's one entry, as a scalar
 __device__ __forceinline__ int seen_keys_of_all(const CrossArgs& a, int b) {
@@ -110,37 +133,147 @@ __device__ __forceinline__ int seen_keys_of_all(const CrossArgs& a, int b) {
 }
 
 // Row r of a kv head's R rows is token r % N of the group's head r / N.
-__device__ __forceinline__ int64_t row_offset(const HeadsView& t, int b, int head0, int r, int N) {
-  const int g = r / N, n = r - g * N;
-  return b * t.sb + (head0 + g) * t.sh + n * t.sn;
+__device__ __forceinline__ int64_t row_offset(const HeadsView& t, int b, int head0, int r, int N, int G) {
+  int g = 0;
+  if (G > 1) g = r / N;
+  return b * t.sb + (head0 + g) * t.sh + (int64_t)(r - g * N) * t.sn;
 }
 
-// B operands of rows base + qt * 16 + i at d = 32s + 8g .. +8; zeros for an absent row or d >= D
+// B operands of rows base + qt * 16 + i at d = 32s + 8g .. +8; zeros for an absent row (null)
+// or d >= D, loaded like the others, so that every call issues as many loads
 template <int D, int QT>
 __device__ __forceinline__ void load_operand(bf16x8 (&op)[QT][Geo16<D>::KS], const uint16_t* const (&rows)[QT], int lane) {
   const int g = lane >> 4;
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt)
+  for (int qt = 0; qt < QT; ++qt) {
+    const uint16_t* row = rows[qt] ? rows[qt] : reinterpret_cast<const uint16_t*>(kZeros);
 #pragma unroll
     for (int s = 0; s < Geo16<D>::KS; ++s) {
       const int d0 = s * 32 + g * 8;
-      if (rows[qt] && d0 < D) op[qt][s] = *reinterpret_cast<const bf16x8*>(rows[qt] + d0);
-      else op[qt][s] = bf16x8{};
+      const uint16_t* p = D % 32 == 0 || d0 < D ? row + d0 : reinterpret_cast<const uint16_t*>(kZeros);
+      op[qt][s] = *reinterpret_cast<const bf16x8*>(p);
     }
+  }
 }
 
-// The keys' places where a mask hides some: 1,024 entries of the list of seen keys in
-// LDS, refilled 512 at a time while the others are in use.
-struct RowRing {
-  static constexpr int kSize = 1024, kHalf = 512;
-  int* ring;
-  const int32_t* list;
-  int end;                       // of the list
-  __device__ __forceinline__ void fill(int first) {
-    for (int e = threadIdx.x; e < kHalf; e += kThreads) ring[(first + e) % kSize] = list[min(first + e, end - 1)];
+// A workgroup's work: some row tiles of a kv head, one after the other, against its keys,
+// or one against a part of them.  Kv heads are the fastest of the three, so that the heads
+// of a token, which lie together in a projection's output, are read at about the same
+// time, and an XCD (every eighth workgroup) has few heads' keys in its L2.
+struct Item {
+  int b, kvh, split, tile, tiles;
+  int count, c0, chunks;         // keys that the entry has, the first 32-key tile and how many
+
+  __device__ __forceinline__ explicit Item(const CrossArgs& a) {
+    const int heads = a.B * a.Hkv, part = blockIdx.x / heads, bh = blockIdx.x - part * heads;
+    const int groups = (a.tiles + a.run - 1) / a.run;
+    split = part / groups;
+    tile = (part - split * groups) * a.run;
+    tiles = min(a.run, a.tiles - tile);
+    b = bh / a.Hkv;
+    kvh = bh - b * a.Hkv;
+    count = seen_keys_of_all(a, b);
+    chunks = (count + CK - 1) / CK;
+    c0 = 0;
+    if (a.splits > 1) {
+      c0 = (int)((int64_t)chunks * split / a.splits);
+      chunks = (int)((int64_t)chunks * (split + 1) / a.splits) - c0;
+    }
   }
-  __device__ __forceinline__ int at(int key) const { return ring[key % kSize]; }
 };
+
+// Feeds tiles of K and V to a workgroup, over and over for one row tile after the other,
+// and says which of a tile's keys are seen: with a mask, a word of `bits` for each tile,
+// read a step ahead as a scalar.
+template <int D, bool MASK>
+struct KeyFeed {
+  using Loader = TileLoader<D>;
+  static constexpr int NUW = Loader::NUW;
+  static constexpr int kLoads = 2 * NUW;         // of a wave for a tile
+  Loader ld;
+  const uint16_t *k0, *v0, *kp, *vp;             // the first tile's first row, and the next one's
+  int keys, left;                                // keys of the part, and from the next tile on
+  uint32_t koff[NUW], voff[NUW];
+  const uint32_t *words0, *words;                // MASK
+  uint32_t word;
+
+  __device__ __forceinline__ void look_up() {
+    if constexpr (MASK) word = *(const __attribute__((address_space(4))) uint32_t*)words;
+    else word = rows_left(left);
+  }
+  __device__ __forceinline__ void rewind() {
+    kp = k0;
+    vp = v0;
+    left = keys;
+    if constexpr (MASK) words = words0;
+  }
+  // (the part has a key)
+  __device__ __forceinline__ void start(const CrossArgs& a, const Item& it, int w, int lane) {
+    ld.init(w, lane);
+    const int64_t row = (int64_t)it.c0 * CK;
+    k0 = static_cast<const uint16_t*>(a.k.p) + it.b * a.k.sb + it.kvh * a.k.sh + row * a.k.sn;
+    v0 = static_cast<const uint16_t*>(a.v.p) + it.b * a.v.sb + it.kvh * a.v.sh + row * a.v.sn;
+    // keys of the next part are not there
+    keys = min(it.count - it.c0 * CK, it.chunks * CK);
+    if constexpr (MASK) words0 = a.bits + (int64_t)it.b * ((a.M + 31) / 32) + it.c0;
+    rewind();
+    look_up();
+    ld.offsets(a.k.sn, koff);
+    ld.offsets(a.v.sn, voff);
+  }
+  // the next tile into LDS, after the last one the first; returns which of its keys are seen
+  __device__ __forceinline__ uint32_t feed(const CrossArgs& a, unsigned ks, unsigned vs) {
+    const uint32_t now = __builtin_amdgcn_readfirstlane(word);
+    ld.load(kp, a.k.sn, koff, now, ks);
+    ld.load(vp, a.v.sn, voff, now, vs);
+    kp += CK * a.k.sn;
+    vp += CK * a.v.sn;
+    left -= CK;
+    if constexpr (MASK) ++words;
+    if (left <= 0) rewind();
+    look_up();
+    return now;
+  }
+};
+
+// A row's D channels to memory as bf16, f times what the lanes hold: lane (g, i) has channels
+// 16dt + 4g .. +4 of row i of a 16-row tile.  Neighbours in g first trade halves of two d
+// tiles, so that a lane writes 16 bytes and four lanes 64 in a row: in 8-byte pieces of 32
+// in a row, 63,240 tokens of 32 heads of 128 over 128 keys took 330 us, so 286.
+template <int D>
+__device__ __forceinline__ void store_row(uint16_t* row, const f32x4* acc, int stride, float f, int g) {
+  constexpr int DT = D / 16;
+#pragma unroll
+  for (int dt = 0; dt < DT; dt += 2) {
+    const f32x4 x = acc[dt * stride];
+    const bf16x2 x0 = cvt2(x[0] * f, x[1] * f), x1 = cvt2(x[2] * f, x[3] * f);
+    if (dt + 1 < DT) {
+      const f32x4 y = acc[(dt + 1) * stride];
+      const bf16x2 y0 = cvt2(y[0] * f, y[1] * f), y1 = cvt2(y[2] * f, y[3] * f);
+      const u32x2 lo = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x0), __builtin_bit_cast(unsigned, y0), false, false);
+      const u32x2 hi = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x1), __builtin_bit_cast(unsigned, y1), false, false);
+      // even g: channels 16dt + 4g .. +8, odd g: 16(dt + 1) + 4(g - 1) .. +8
+      if (row) *reinterpret_cast<u32x4*>(row + (dt + (g & 1)) * 16 + 4 * (g & 2)) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+    } else if (row) {
+      const bf16x4 z = {x0[0], x0[1], x1[0], x1[1]};
+      *reinterpret_cast<bf16x4*>(row + dt * 16 + 4 * g) = z;
+    }
+  }
+}
+
+// logits of a tile's hidden keys to -inf
+template <int QT>
+__device__ __forceinline__ void hide(f32x4 (&s)[2][QT], uint32_t bits, int lane) {
+  const uint32_t mine = bits >> (4 * (lane >> 4));
+#pragma unroll
+  for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (!(mine >> (k2 * 16 + r) & 1)) {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) s[k2][qt][r] = -INFINITY;
+      }
+}
 
 }  // namespace cross
 }  // namespace sva

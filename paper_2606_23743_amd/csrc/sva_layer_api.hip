@@ -99,12 +99,13 @@ int cross_sizes(const sva_cross* p, bool mask, bool grad, sva::CrossArgs* a, sva
   if (!(a->scale >= FLT_MIN && a->scale_log2 <= FLT_MAX)) return SVA_ERR_INVALID_ARG;
   *s = (grad ? sva::cross_grad_shape : sva::cross_shape)(a->B, a->Hkv, a->G, a->N, a->M, a->D, mask);
   a->tiles = s->tiles;
+  a->run = s->run;
   a->splits = s->splits;
   a->key_tiles = s->key_tiles;
   a->row_splits = s->row_splits;
   // a launch has fewer than 2^32 threads, 256 (join: a row each) a workgroup
   const int64_t heads = (int64_t)a->B * a->Hkv, most = ((int64_t)1 << 24) - 1;
-  const int64_t wgs = heads * s->tiles * s->splits, kv_wgs = heads * s->key_tiles * s->row_splits;
+  const int64_t wgs = heads * ((s->tiles + s->run - 1) / s->run) * s->splits, kv_wgs = heads * s->key_tiles * s->row_splits;
   if (wgs > most || kv_wgs > most || (s->splits > 1 && heads * a->R > most)) return SVA_ERR_SHAPE;
   a->wgs = (int)wgs;
   a->kv_wgs = (int)kv_wgs;
@@ -137,7 +138,7 @@ int check_workspace(void* workspace, size_t bytes, size_t need) {
 
 void place_workspace(void* workspace, const sva::CrossShape& s, sva::CrossArgs* a) {
   unsigned char* w = static_cast<unsigned char*>(workspace);
-  a->rows = reinterpret_cast<int32_t*>(w + s.rows_at);
+  a->bits = reinterpret_cast<uint32_t*>(w + s.bits_at);
   a->seen = reinterpret_cast<int32_t*>(w + s.seen_at);
   a->stat = reinterpret_cast<float2*>(w + s.stat_at);
   a->stat_l = reinterpret_cast<float*>(w + s.stat_l_at);
