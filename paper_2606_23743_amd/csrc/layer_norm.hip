@@ -4,16 +4,21 @@
 //   dw = sum of dy xhat, dbias = sum of dy, over all rows or an entry's
 // with w = unit + weight (unit 1: a scale around one, as adaptive norms have it).
 //
-// Bound by HBM: an element is read (x; dy) and written once and costs some ten
-// operations.  A row stays in registers from its load to its store, in pieces of
-// eight elements: 16 or 32 lanes or a wave hold a short row, a whole workgroup a
-// longer one, V pieces a lane.  A workgroup takes rows of one batch entry, so the
-// weights are loaded once, and while it reduces a row the next one is on its way.
-// A wave forms mean and squared deviations of its own part by two sums over its
-// lanes; the waves' parts are joined as (count, mean, M2), one barrier a row, so
-// no difference of large sums is ever taken.  The weights' gradients are summed
-// over a workgroup's rows in registers, written once per workgroup and added in a
-// fixed order by a second launch: the same call gives the same bits.
+// Bound by HBM, and next to it by vector operations (an element is read and written once;
+// 16 lanes a clock leave some twenty operations for it).  A row stays in registers from its
+// load to its store, in pieces of eight elements.  Forward: 16 or 32 lanes or a wave hold a
+// row of up to 6,144 channels, and no wave waits for another; longer ones a workgroup.
+// Gradients: a wave up to 1,024, then a workgroup, whose lanes keep the sums of their
+// columns for the weights' gradients in registers.  A workgroup takes rows of one batch
+// entry, so the weights are loaded once; the next rows are on their way while one is worked
+// on, and workgroups are a whole number per CU, each with as many rows.  Means are sums of
+// differences or of the elements in a tree, squares are of deviations from the mean, so no
+// difference of large sums is ever taken.  The weights' gradients are written once per
+// workgroup and added in a fixed order by a second launch: the same call gives the same bits.
+//
+// 63,240 x 4,096 bf16: 207 us (5.0 TB/s), gradients 286 (5.4); 65,520 x 2,240: 116 and 171;
+// 23,403 x 1,001 float32: 42 and 60.  With a workgroup to every row and one row ahead the
+// first took 237 and 358, the second 185 and 240.
 #include <type_traits>
 
 #include "norm_args.h"
@@ -134,6 +139,12 @@ __device__ __forceinline__ float lanes_sum(float x) {
   return x;
 }
 
+// weight c as float32: `none` where there are no weights or no channel c
+__device__ __forceinline__ float weight_at(const void* w, bool bf16, int64_t at, float none, float add, int c, int C) {
+  if (!w || c >= C) return none;
+  return add + (bf16 ? wide(static_cast<const uint16_t*>(w)[at + c]) : static_cast<const float*>(w)[at + c]);
+}
+
 // The weights of a lane's pieces as float32 (ones plus the offset where there are none).
 template <int V>
 __device__ __forceinline__ void load_weights(const void* w, bool bf16, int64_t at, float none, float add, int lane0, int step,
@@ -141,11 +152,7 @@ __device__ __forceinline__ void load_weights(const void* w, bool bf16, int64_t a
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = (lane0 + v * step) * E + e;
-      out[v][e] = none;
-      if (w && c < C) out[v][e] = add + (bf16 ? wide(static_cast<const uint16_t*>(w)[at + c]) : static_cast<const float*>(w)[at + c]);
-    }
+    for (int e = 0; e < E; ++e) out[v][e] = weight_at(w, bf16, at, none, add, (lane0 + v * step) * E + e, C);
 }
 
 // How a launch's lanes take rows.  L lanes hold a row (L = 0: the workgroup), V pieces
@@ -172,8 +179,138 @@ __device__ __forceinline__ void load_row(const Elem<F32>* row, int lane, int ste
   }
 }
 
-template <bool F32, bool ALIGNED, int L, int V, int T>
+// a tree of eight
+__device__ __forceinline__ float sum8(const float (&f)[E]) {
+  return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+}
+
+// Rows of up to 6,144 channels: L lanes of a wave hold one, V pieces a lane, and no wave
+// waits for another.  Vector operations bound it as much as HBM does (16 lanes a clock,
+// some seven operations an element), so the row's deviations stay in registers, and the
+// weights of longer rows, which would crowd them out, lie in LDS.
+template <bool F32, bool ALIGNED, int L, int V>
+__global__ __launch_bounds__(kNormThreads) void norm_wave_kernel(NormArgs a) {
+  constexpr int PF = V <= 2 ? 4 : V <= 4 ? 2 : 1;  // rows on their way
+  constexpr bool IN_LDS = V > 1;
+  __shared__ float4 lds_w[IN_LDS ? 2 * V * 2 * 64 : 1];
+  const int C = a.C, b = blockIdx.x / a.parts, part = blockIdx.x - b * a.parts;
+  const int lane = threadIdx.x % L;
+  const Elem<F32>* xs = static_cast<const Elem<F32>*>(a.x.p) + b * a.x.sb;
+  Elem<F32>* ys = static_cast<Elem<F32>*>(a.y.p) + b * a.y.sb;
+  const int stride = a.parts * (kNormThreads / L);
+  int n = part * (kNormThreads / L) + threadIdx.x / L;
+
+  Piece<F32> ring[PF][V];
+#pragma unroll
+  for (int u = 0; u < PF; ++u)
+    if (n + (int64_t)u * stride < a.N) load_row<F32, ALIGNED, V>(xs + (n + (int64_t)u * stride) * a.x.sn, lane, L, C, ring[u]);
+
+  float w[IN_LDS ? 1 : V][E], bias[IN_LDS ? 1 : V][E];
+  if constexpr (IN_LDS) {
+    // as halves of pieces, each in the order of the lanes: no two of them on one bank
+    for (int i = threadIdx.x; i < V * 2 * 64; i += kNormThreads) {
+      const int c = (i / 128 * 64 + i % 64) * E + i / 64 % 2 * 4;
+      float q[2][4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        q[0][e] = weight_at(a.w, a.w_bf16, b * a.w_b, 1.0f, a.unit, c + e, C);
+        q[1][e] = weight_at(a.bias, a.w_bf16, b * a.bias_b, 0.0f, 0.0f, c + e, C);
+      }
+      lds_w[i] = make_float4(q[0][0], q[0][1], q[0][2], q[0][3]);
+      lds_w[V * 2 * 64 + i] = make_float4(q[1][0], q[1][1], q[1][2], q[1][3]);
+    }
+    __syncthreads();
+  } else {
+    load_weights<V>(a.w, a.w_bf16, b * a.w_b, 1.0f, a.unit, lane, L, C, w);
+    load_weights<V>(a.bias, a.w_bf16, b * a.bias_b, 0.0f, 0.0f, lane, L, C, bias);
+  }
+  const float inv_c = 1.0f / (float)C;
+
+  // zeros behind the row's end, in the one piece of its lanes that may hold it
+  auto clear_tail = [&](float (&f)[E], int v) {
+    if (ALIGNED || (v + 1) * L * E <= C) return;
+    int left = C - (lane + v * L) * E;
+    asm volatile("" : "+v"(left));             // (not eight masks kept from row to row)
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[e] = e < left ? f[e] : 0.0f;
+  };
+  auto row = [&](Piece<F32> (&x)[V]) {
+    // Sums of float32 rows are of differences from the first element: a mean far from zero
+    // then costs the sum no digits (bf16 rows have none that it could cost).
+    float f[V][E], sum = 0.0f, first = 0.0f;
+    if constexpr (F32) first = __shfl(__uint_as_float(x[0].w[0]), 0, L);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (lane + v * L) * E;
+      widen<F32>(x[v], f[v]);
+      if (c < C) {
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[v][e] -= first;
+          clear_tail(f[v], v);
+        }
+        sum += sum8(f[v]);
+      }
+    }
+    const float off = lanes_sum<L>(sum) * inv_c, mean = first + off;
+    float m2 = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (lane + v * L) * E;
+      if (c < C) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[v][e] -= off;
+        clear_tail(f[v], v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) m2 = fmaf(f[v][e], f[v][e], m2);
+      }
+    }
+    const float rstd = 1.0f / sqrtf(lanes_sum<L>(m2) * inv_c + a.eps);
+    if (lane == 0) {
+      if (a.mean) a.mean[(int64_t)b * a.N + n] = mean;
+      if (a.rstd) a.rstd[(int64_t)b * a.N + n] = rstd;
+    }
+    Elem<F32>* y = ys + n * a.y.sn;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (lane + v * L) * E;
+      if (c < C) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float wq[4], bq[4];
+          if constexpr (IN_LDS) {
+            const float4 p = lds_w[(v * 2 + h) * 64 + lane], q = lds_w[V * 2 * 64 + (v * 2 + h) * 64 + lane];
+            wq[0] = p.x, wq[1] = p.y, wq[2] = p.z, wq[3] = p.w;
+            bq[0] = q.x, bq[1] = q.y, bq[2] = q.z, bq[3] = q.w;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              wq[e] = w[v][4 * h + e];
+              bq[e] = bias[v][4 * h + e];
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[v][4 * h + e] = fmaf(f[v][4 * h + e] * rstd, wq[e], bq[e]);
+        }
+        store_piece<F32, ALIGNED>(y + c, narrow<F32>(f[v]), C - c);
+      }
+    }
+    const int64_t later = n + (int64_t)PF * stride;
+    if (later < a.N) load_row<F32, ALIGNED, V>(xs + later * a.x.sn, lane, L, C, x);
+    n += stride;
+  };
+  while (n < a.N) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u)
+      if (n < a.N) row(ring[u]);
+  }
+}
+
+// Longer rows: a workgroup holds one.  A wave forms mean and squared deviations of its own
+// part; the waves' parts are joined as (count, mean, M2), one barrier a row.
+template <bool F32, bool ALIGNED, int V, int T>
 __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
+  constexpr int L = 0, PF = T > 512 ? 1 : 2;
   const Place<L> at;
   const int C = a.C, b = blockIdx.x / a.parts, part = blockIdx.x - b * a.parts;
   __shared__ float2 joined[2][16];            // (mean, M2) of the waves' parts, two rows in turn
@@ -194,13 +331,15 @@ __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
   }
   const float inv_c = 1.0f / (float)C, inv_mine = mine ? 1.0f / (float)mine : 0.0f;
 
-  Piece<F32> x[V], next[V];
+  // A row's loads go out PF rows ahead of its use: one row ahead left HBM waiting
+  Piece<F32> ring[PF][V];
   const int stride = a.parts * at.groups;
   int n = part * at.groups + at.group, turn = 0;
-  if (n < a.N) load_row<F32, ALIGNED, V>(xs + n * a.x.sn, at.lane, at.step, C, x);
+#pragma unroll
+  for (int u = 0; u < PF; ++u)
+    if (n + (int64_t)u * stride < a.N) load_row<F32, ALIGNED, V>(xs + (n + (int64_t)u * stride) * a.x.sn, at.lane, at.step, C, ring[u]);
   // (a workgroup's lanes are at the same row, or there is no barrier below)
-  for (; n < a.N; n += stride, turn ^= 1) {
-    if (n + stride < a.N) load_row<F32, ALIGNED, V>(xs + (n + stride) * a.x.sn, at.lane, at.step, C, next);
+  auto row = [&](Piece<F32> (&x)[V]) {
     float sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -263,16 +402,25 @@ __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
         for (int e = 0; e < E; ++e) f[e] = fmaf((f[e] - mean) * rstd, w[v][e], bias[v][e]);
         store_piece<F32, ALIGNED>(y + c, narrow<F32>(f), C - c);
       }
-      x[v] = next[v];
     }
+    const int64_t later = n + (int64_t)PF * stride;
+    if (later < a.N) load_row<F32, ALIGNED, V>(xs + later * a.x.sn, at.lane, at.step, C, x);
+    n += stride;
+    turn ^= 1;
+  };
+  while (n < a.N) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u)
+      if (n < a.N) row(ring[u]);
   }
 }
 
-template <bool F32, bool ALIGNED, int L, int V, int T>
+template <bool F32, bool ALIGNED, int L, int V, int T, int R>
 __global__ __launch_bounds__(T) void norm_grad_kernel(NormArgs a) {
+  constexpr int PF = T > 512 ? 1 : R == 2 ? 2 : F32 ? 2 : 3;   // times R rows on their way
   const Place<L> at;
   const int C = a.C, b = blockIdx.x / a.parts, part = blockIdx.x - b * a.parts;
-  __shared__ float2 joined[2][16];
+  __shared__ float2 joined[2][R][16];
 
   float w[V][E], dw[V][E] = {}, db[V][E] = {};
   load_weights<V>(a.w, a.w_bf16, b * a.w_b, 1.0f, a.unit, at.lane, at.step, C, w);
@@ -284,72 +432,92 @@ __global__ __launch_bounds__(T) void norm_grad_kernel(NormArgs a) {
   const int waves = blockDim.x / 64, wave = threadIdx.x / 64;
   const float inv_c = 1.0f / (float)C;
 
-  Piece<F32> x[V], g[V], xn[V], gn[V];
-  float mean = 0.0f, rstd = 0.0f, mean_n = 0.0f, rstd_n = 0.0f;
+  struct Row {
+    Piece<F32> x[V], g[V];
+    float mean, rstd;
+  };
+  Row ring[PF][R];
   const int stride = a.parts * at.groups;
   int n = part * at.groups + at.group, turn = 0;
-  if (n < a.N) {
-    load_row<F32, ALIGNED, V>(xs + n * a.x.sn, at.lane, at.step, C, x);
-    load_row<F32, ALIGNED, V>(gs + n * a.dy.sn, at.lane, at.step, C, g);
-    mean = means[n];
-    rstd = rstds[n];
-  }
-  for (; n < a.N; n += stride, turn ^= 1) {
-    if (n + stride < a.N) {
-      load_row<F32, ALIGNED, V>(xs + (n + stride) * a.x.sn, at.lane, at.step, C, xn);
-      load_row<F32, ALIGNED, V>(gs + (n + stride) * a.dy.sn, at.lane, at.step, C, gn);
-      mean_n = means[n + stride];
-      rstd_n = rstds[n + stride];
-    }
-    float s1 = 0.0f, s2 = 0.0f;
+  // R rows a stride apart; one that is not there is zeros, and adds nothing
+  auto load = [&](int64_t n, Row (&r)[R]) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float f[E], d[E];
-      widen<F32>(x[v], f);
-      widen<F32>(g[v], d);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        // past the row's end dy is zero, and so are all four
-        const float xh = (f[e] - mean) * rstd, gw = d[e] * w[v][e];
-        dw[v][e] = fmaf(d[e], xh, dw[v][e]);
-        db[v][e] += d[e];
-        s1 += gw;
-        s2 = fmaf(gw, xh, s2);
+    for (int k = 0; k < R; ++k) {
+      const int64_t m = n + (int64_t)k * stride;
+      if (m < a.N) {
+        load_row<F32, ALIGNED, V>(xs + m * a.x.sn, at.lane, at.step, C, r[k].x);
+        load_row<F32, ALIGNED, V>(gs + m * a.dy.sn, at.lane, at.step, C, r[k].g);
+        r[k].mean = means[m];
+        r[k].rstd = rstds[m];
+      } else {
+        r[k] = Row{};
       }
     }
-    s1 = lanes_sum<L ? L : 64>(s1);
-    s2 = lanes_sum<L ? L : 64>(s2);
-    if constexpr (L == 0) {
-      if (threadIdx.x % 64 == 0) joined[turn][wave] = make_float2(s1, s2);
-      __syncthreads();
-      s1 = s2 = 0.0f;
-      for (int i = 0; i < waves; ++i) {
-        s1 += joined[turn][i].x;
-        s2 += joined[turn][i].y;
-      }
-    }
-    s1 *= inv_c;
-    s2 *= inv_c;
-    Elem<F32>* out = outs + n * a.y.sn;
+  };
+  auto rows = [&](Row (&r)[R]) {
+    float s1[R], s2[R], f[R][V][E], d[R][V][E];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (at.lane + v * at.step) * E;
-      if (c < C) {
-        float f[E], d[E];
-        widen<F32>(x[v], f);
-        widen<F32>(g[v], d);
+    for (int k = 0; k < R; ++k) {
+      s1[k] = s2[k] = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        widen<F32>(r[k].x[v], f[k][v]);
+        widen<F32>(r[k].g[v], d[k][v]);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float xh = (f[e] - mean) * rstd;
-          f[e] = rstd * (fmaf(d[e], w[v][e], -s1) - xh * s2);
+          // past the row's end dy is zero, and so are all four
+          f[k][v][e] = (f[k][v][e] - r[k].mean) * r[k].rstd;       // xhat
+          dw[v][e] = fmaf(d[k][v][e], f[k][v][e], dw[v][e]);
+          db[v][e] += d[k][v][e];
+          d[k][v][e] *= w[v][e];                                   // g
+          s1[k] += d[k][v][e];
+          s2[k] = fmaf(d[k][v][e], f[k][v][e], s2[k]);
         }
-        store_piece<F32, ALIGNED>(out + c, narrow<F32>(f), C - c);
       }
-      x[v] = xn[v];
-      g[v] = gn[v];
+      s1[k] = lanes_sum<L ? L : 64>(s1[k]);
+      s2[k] = lanes_sum<L ? L : 64>(s2[k]);
     }
-    mean = mean_n;
-    rstd = rstd_n;
+    if constexpr (L == 0) {
+      if (threadIdx.x % 64 == 0) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) joined[turn][k][wave] = make_float2(s1[k], s2[k]);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        s1[k] = s2[k] = 0.0f;
+        for (int i = 0; i < waves; ++i) {
+          s1[k] += joined[turn][k][i].x;
+          s2[k] += joined[turn][k][i].y;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int64_t m = n + (int64_t)k * stride;
+      if (m >= a.N) continue;
+      const float m1 = s1[k] * inv_c, m2 = s2[k] * inv_c;
+      Elem<F32>* out = outs + m * a.y.sn;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int c = (at.lane + v * at.step) * E;
+        if (c < C) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[k][v][e] = r[k].rstd * ((d[k][v][e] - m1) - f[k][v][e] * m2);
+          store_piece<F32, ALIGNED>(out + c, narrow<F32>(f[k][v]), C - c);
+        }
+      }
+    }
+    load(n + (int64_t)PF * R * stride, r);
+    n += R * stride;
+    turn ^= 1;
+  };
+#pragma unroll
+  for (int u = 0; u < PF; ++u) load(n + (int64_t)u * R * stride, ring[u]);
+  while (n < a.N) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u)
+      if (n < a.N) rows(ring[u]);
   }
   if (!a.dw && !a.db) return;
   // an entry's only workgroup has its sums whole
@@ -415,22 +583,28 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, f
 
 template <bool F32, bool ALIGNED>
 void launch_as(const NormArgs& a, const NormShape& s, bool grad, hipStream_t stream) {
-  auto go = [&](auto lanes, auto pieces, auto threads) {
-    constexpr int L = decltype(lanes)::value, V = decltype(pieces)::value, T = decltype(threads)::value;
-    if (grad) hipLaunchKernelGGL((norm_grad_kernel<F32, ALIGNED, L, V, T>), dim3(a.B * a.parts), dim3(s.threads), 0, stream, a);
-    else hipLaunchKernelGGL((norm_kernel<F32, ALIGNED, L, V, T>), dim3(a.B * a.parts), dim3(s.threads), 0, stream, a);
-  };
   using std::integral_constant;
-  integral_constant<int, 0> wg;
-  integral_constant<int, 1> one;
-  integral_constant<int, 2> two;
-  integral_constant<int, kNormThreads> few;
-  if (s.lanes == 16) go(integral_constant<int, 16>{}, one, few);
-  else if (s.lanes == 32) go(integral_constant<int, 32>{}, one, few);
-  else if (s.lanes == 64) go(integral_constant<int, 64>{}, one, few);
-  else if (s.pieces == 1) go(wg, one, few);
-  else if (s.threads <= 512) go(wg, two, integral_constant<int, 512>{});
-  else go(wg, two, integral_constant<int, 1024>{});
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.B * a.parts), dim3(s.threads), 0, stream, a); };
+  if (grad) {
+    if (s.lanes == 16) go(norm_grad_kernel<F32, ALIGNED, 16, 1, kNormThreads, 1>);
+    else if (s.lanes == 32) go(norm_grad_kernel<F32, ALIGNED, 32, 1, kNormThreads, 1>);
+    else if (s.lanes == 64 && s.pieces == 1) go(norm_grad_kernel<F32, ALIGNED, 64, 1, kNormThreads, 1>);
+    else if (s.lanes == 64) go(norm_grad_kernel<F32, ALIGNED, 64, 2, kNormThreads, 1>);
+    else if (s.pieces == 1) go(norm_grad_kernel<F32, ALIGNED, 0, 1, 512, 2>);
+    else if (s.threads <= 512) go(norm_grad_kernel<F32, ALIGNED, 0, 2, 512, 1>);
+    else go(norm_grad_kernel<F32, ALIGNED, 0, 2, 1024, 1>);
+  } else if (s.lanes) {
+    if (s.lanes == 16) go(norm_wave_kernel<F32, ALIGNED, 16, 1>);
+    else if (s.lanes == 32) go(norm_wave_kernel<F32, ALIGNED, 32, 1>);
+    else if (s.pieces == 1) go(norm_wave_kernel<F32, ALIGNED, 64, 1>);
+    else if (s.pieces == 2) go(norm_wave_kernel<F32, ALIGNED, 64, 2>);
+    else if (s.pieces == 4) go(norm_wave_kernel<F32, ALIGNED, 64, 4>);
+    else if (s.pieces == 8) go(norm_wave_kernel<F32, ALIGNED, 64, 8>);
+    else go(norm_wave_kernel<F32, ALIGNED, 64, 12>);
+  } else {
+    if (s.threads <= 512) go(norm_kernel<F32, ALIGNED, 2, 512>);
+    else go(norm_kernel<F32, ALIGNED, 2, 1024>);
+  }
 }
 
 hipError_t launch(const NormArgs& a, const NormShape& s, bool grad, hipStream_t stream) {
@@ -449,18 +623,28 @@ hipError_t launch(const NormArgs& a, const NormShape& s, bool grad, hipStream_t 
 NormShape norm_shape(int B, int N, int C, bool grad, bool per_entry) {
   NormShape s{};
   const int pieces = (C + E - 1) / E;
+  int per_cu;                                   // workgroups of a CU, a whole number: each takes as many rows
+  s.threads = kNormThreads;
   if (pieces <= 64) {
     s.lanes = pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64;
     s.pieces = 1;
-    s.threads = kNormThreads;
+    per_cu = grad ? 3 : 6;
+  } else if (grad && pieces <= 2 * 64) {
+    s.lanes = 64;
+    s.pieces = 2;
+    per_cu = 3;
+  } else if (!grad && pieces <= 12 * 64) {
+    s.lanes = 64;
+    s.pieces = pieces <= 2 * 64 ? 2 : pieces <= 4 * 64 ? 4 : pieces <= 8 * 64 ? 8 : 12;
+    per_cu = s.pieces == 2 ? 6 : s.pieces == 4 ? 4 : s.pieces == 8 ? 3 : 2;
   } else {
-    s.lanes = 0;
-    s.pieces = pieces <= 256 ? 1 : 2;
+    s.pieces = pieces <= 384 ? 1 : 2;
     s.threads = ((pieces + s.pieces - 1) / s.pieces + 63) / 64 * 64;
+    per_cu = (grad ? 704 : 2048) / s.threads;
+    if (per_cu < 1) per_cu = 1;
   }
   const int rows = s.lanes ? kNormThreads / s.lanes : 1;     // of a workgroup at a time
-  const int64_t full = 256 * (grad ? 4 : 8) * 256 / s.threads;   // workgroups that fill the card
-  int64_t parts = (full + B - 1) / B;
+  int64_t parts = (256 * per_cu + B - 1) / B;
   const int64_t most = ((int64_t)N + rows - 1) / rows;
   if (parts > most) parts = most;
   s.parts = (int)parts;

@@ -36,7 +36,7 @@ struct NormArgs {
 // How a call's rows are held, and its workspace.
 struct NormShape {
   int lanes;                     // of a row: 16, 32, 64, or 0: a workgroup's
-  int pieces;                    // of a lane
+  int pieces;                    // of a lane, at most
   int threads, parts;
   size_t ws_bytes;
 };
