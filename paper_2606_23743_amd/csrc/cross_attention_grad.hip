@@ -45,10 +45,11 @@ void cross_grad_rows_kernel(CrossArgs a) {
 
   // Q and dO of the wave's rows, their lse and delta
   bf16x8 qop[QT][G16::KS], gop[QT][G16::KS];
-  float lse2[QT], delta[QT];
+  float lse2[QT], delta[QT], excess[QT];
+  bf16x8 oop[QT][G16::KS];
+  float lse[QT];
   auto load_rows = [&](int tile) {
     const uint16_t *qrow[QT], *grow[QT], *orow[QT];
-    float lse[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       const int r = row_of(tile, qt);
@@ -61,10 +62,11 @@ void cross_grad_rows_kernel(CrossArgs a) {
         lse[qt] = a.lse[bh * a.R + r];
       }
     }
-    bf16x8 oop[QT][G16::KS];
     load_operand<D>(qop, qrow, lane);
     load_operand<D>(gop, grow, lane);
     load_operand<D>(oop, orow, lane);
+  };
+  auto take_rows = [&]() {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       float s = 0.0f;
@@ -75,8 +77,17 @@ void cross_grad_rows_kernel(CrossArgs a) {
       delta[qt] = quad_sum(s);
       // a row that saw no key has P = 0 everywhere
       lse2[qt] = lse[qt] == -INFINITY ? INFINITY : lse[qt] * 1.4426950408889634074f;
+      excess[qt] = 0.0f;
+    }
+  };
+  // A row's dS sum to zero; what they sum to, here, is what out's rounding to bf16 took from
+  // delta, and the second launch gets delta with it.  (dQ has been summed with the other.)
+  auto put_stat = [&](int tile) {
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      const float d = a.splits == 1 ? delta[qt] + quad_sum(excess[qt]) : delta[qt];
       const int r = row_of(tile, qt);
-      if (it.split == 0 && g == 0 && r < a.R) a.stat[bh * a.R + r] = make_float2(lse2[qt], delta[qt]);
+      if (it.split == 0 && g == 0 && r < a.R) a.stat[bh * a.R + r] = make_float2(lse2[qt], d);
     }
   };
   f32x4 dq[G16::DT][QT] = {};
@@ -100,6 +111,8 @@ void cross_grad_rows_kernel(CrossArgs a) {
   if (it.chunks == 0) {            // no key: zeros
     for (int t = 0; t < it.tiles; ++t) {
       load_rows(it.tile + t);
+      take_rows();
+      put_stat(it.tile + t);       // (other parts may have keys)
       store(it.tile + t);
     }
     return;
@@ -113,6 +126,7 @@ void cross_grad_rows_kernel(CrossArgs a) {
 #pragma unroll
   for (int c = 0; c < PD; ++c) seen[c] = fetch(c);
   load_rows(it.tile);
+  take_rows();
 
   int koff[G16::KS], voff[G16::DT];
   operand_offsets<D>(lane, koff, voff);
@@ -144,18 +158,26 @@ void cross_grad_rows_kernel(CrossArgs a) {
         for (int e = 0; e < 2; ++e) {
           const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e], sl2, -lse2[qt]));
           const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e + 1], sl2, -lse2[qt]));
-          const bf16x2 x = cvt2(p0 * (dp[k2][qt][2 * e] - delta[qt]), p1 * (dp[k2][qt][2 * e + 1] - delta[qt]));
-          wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, x);
+          const float d0 = p0 * (dp[k2][qt][2 * e] - delta[qt]), d1 = p1 * (dp[k2][qt][2 * e + 1] - delta[qt]);
+          excess[qt] += d0 + d1;
+          wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, cvt2(d0, d1));
         }
       dsop[qt] = __builtin_bit_cast(bf16x8, wv);
     }
+    // the next rows are on their way during the last product and the result's stores
+    const bool last = c + 1 == it.chunks;
+    if (last) {
+      put_stat(tile);
+      if (tile + 1 < end) load_rows(tile + 1);
+    }
     pv16<D>(dsop, kt, voff, dq);
     st = (st + 1) % NST;
-    if (++c == it.chunks) {
+    ++c;
+    if (last) {
       store(tile);
       c = 0;
       if (++tile == end) break;
-      load_rows(tile);
+      take_rows();
     }
   }
   wait_vmcnt<0>();                 // no load may still target this workgroup's LDS
@@ -242,8 +264,7 @@ void cross_grad_keys_kernel(CrossArgs a) {
         bases();
       }
     };
-    int koff[G16::KS], voff[G16::DT];
-    operand_offsets<D>(lane, koff, voff);
+    const Places<D> at(lane);
 #pragma unroll
     for (int c = 0; c < PD; ++c) fetch(c);
     int st = 0;
@@ -253,35 +274,35 @@ void cross_grad_keys_kernel(CrossArgs a) {
       wg_barrier();                                  // and every wave is done with the one before
       fetch((st + PD) % NST);
       if (key0 < count) {
-        const unsigned char *qt = &Qs[0][0] + st * CT, *gt = &Gs[0][0] + st * CT;
+        const unsigned qt = qs_base + st * CT, gt = gs_base + st * CT;
         const float4* stat = reinterpret_cast<const float4*>(&Ss[st][0]);   // rows 2x and 2x + 1
-        f32x4 s[2][KT], dp[2][KT];
-        qk16<D>(s, qt, koff, kop);
-        qk16<D>(dp, gt, koff, vop);
+        // half a tile's rows at a time: S and dP of all 32 would crowd out what is read ahead
         bf16x8 pop[KT], dsop[KT];
         u32x4 pw[KT], dw[KT];
 #pragma unroll
-        for (int r2 = 0; r2 < 2; ++r2)
+        for (int x = 0; x < 2; ++x) {
+          f32x4 s[KT], dp[KT];
+          rows_times_half<D>(s, qt + x * 16 * Geo<D>::RB, at, kop);
+          rows_times_half<D>(dp, gt + x * 16 * Geo<D>::RB, at, vop);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float4 x = stat[r2 * 8 + 2 * g + e];     // (lse, delta) of two rows
+            const float4 z = stat[x * 8 + 2 * g + e];      // (lse, delta) of two rows
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r2][kt][2 * e], sl2, -x.x));
-              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r2][kt][2 * e + 1], sl2, -x.z));
-              const bf16x2 p = cvt2(p0, p1);
-              const bf16x2 d = cvt2(p0 * (dp[r2][kt][2 * e] - x.y), p1 * (dp[r2][kt][2 * e + 1] - x.w));
-              pw[kt][r2 * 2 + e] = __builtin_bit_cast(unsigned, p);
-              dw[kt][r2 * 2 + e] = __builtin_bit_cast(unsigned, d);
+              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][2 * e], sl2, -z.x));
+              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][2 * e + 1], sl2, -z.z));
+              pw[kt][x * 2 + e] = __builtin_bit_cast(unsigned, cvt2(p0, p1));
+              dw[kt][x * 2 + e] = __builtin_bit_cast(unsigned, cvt2(p0 * (dp[kt][2 * e] - z.y), p1 * (dp[kt][2 * e + 1] - z.w)));
             }
           }
+        }
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
           pop[kt] = __builtin_bit_cast(bf16x8, pw[kt]);
           dsop[kt] = __builtin_bit_cast(bf16x8, dw[kt]);
         }
-        pv16<D>(pop, gt, voff, dv);
-        pv16<D>(dsop, qt, voff, dk);
+        cols_times<D>(pop, gt, at, dv);
+        cols_times<D>(dsop, qt, at, dk);
       }
       st = (st + 1) % NST;
     }

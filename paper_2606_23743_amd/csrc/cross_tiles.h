@@ -36,6 +36,77 @@ __device__ __forceinline__ void operand_offsets(int lane, int (&koff)[Geo16<D>::
     voff[dt] = r1 * G::RB + (swz<G::NCH>(r1, 2 * dt + ((i & 3) >> 1)) << 4) + (i & 1) * 8;
 }
 
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+
+// A lane's place in a tile, for the row operands (row i at channels 8g .. +8) and for the
+// transpose reads (rows 4g.. at channels 0..).  Step s of the rows is at place ^ s << 6,
+// d tile dt at place ^ dt << 5, 16 rows further the swizzle is the same: one register
+// holds them all.
+template <int D>
+struct Places {
+  unsigned row, col;
+  __device__ __forceinline__ explicit Places(int lane) {
+    using G = Geo<D>;
+    const int g = lane >> 4, i = lane & 15, r1 = 4 * g + (i >> 2);
+    row = i * G::RB + (swz<G::NCH>(i, g) << 4);
+    col = r1 * G::RB + (swz<G::NCH>(r1, (i & 3) >> 1) << 4) + (i & 1) * 8;
+  }
+};
+
+// S = rows of the tile at LDS address `tile` times the rows in registers: for the tile's
+// rows 16x + 4g + r and the register rows 16qt + i, sum over d
+template <int D, int QT>
+__device__ __forceinline__ void rows_times(f32x4 (&s)[2][QT], unsigned tile, const Places<D>& at,
+                                           const bf16x8 (&op)[QT][Geo16<D>::KS]) {
+  using G = Geo<D>;
+  const unsigned p = tile + at.row;
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) s[x][qt] = f32x4{};
+#pragma unroll
+  for (int k = 0; k < Geo16<D>::KS; ++k)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const bf16x8 row = *(lds_bf16x8*)(size_t)((p ^ (k << 6)) + x * 16 * G::RB);
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) s[x][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, op[qt][k], s[x][qt], 0, 0, 0);
+    }
+}
+
+// 16 of a tile's rows times those in registers
+template <int D, int QT>
+__device__ __forceinline__ void rows_times_half(f32x4 (&s)[QT], unsigned tile, const Places<D>& at,
+                                                const bf16x8 (&op)[QT][Geo16<D>::KS]) {
+  const unsigned p = tile + at.row;
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) s[qt] = f32x4{};
+#pragma unroll
+  for (int k = 0; k < Geo16<D>::KS; ++k) {
+    const bf16x8 row = *(lds_bf16x8*)(size_t)(p ^ (k << 6));
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) s[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, op[qt][k], s[qt], 0, 0, 0);
+  }
+}
+
+// acc += the tile's columns times the weights in registers, over its 32 rows in the order
+// of attn_w16.h
+template <int D, int QT>
+__device__ __forceinline__ void cols_times(const bf16x8 (&wop)[QT], unsigned tile, const Places<D>& at,
+                                           f32x4 (&acc)[Geo16<D>::DT][QT]) {
+  using G = Geo<D>;
+  const unsigned p = tile + at.col;
+#pragma unroll
+  for (int dt = 0; dt < Geo16<D>::DT; ++dt) {
+    const unsigned q = p ^ (dt << 5);
+    const u32x2 lw = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)q));
+    const u32x2 hw = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)(q + 16 * G::RB)));
+    const bf16x8 col = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], hw[0], hw[1]});
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) acc[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(col, wop[qt], acc[dt][qt], 0, 0, 0);
+  }
+}
+
 // What rows that are not there and channels past D are loaded from.
 __device__ const uint4 kZeros[16] = {};
 __device__ const float kInf[2] = {INFINITY, 0.0f};   // a row's lse and delta

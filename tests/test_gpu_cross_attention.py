@@ -126,7 +126,9 @@ class Case:
             lost = TINY * (1 + np.abs(go) @ np.abs(v).T + (np.abs(go) * np.abs(o64[b, h])).sum(-1, keepdims=True))
             ds_err = p * d_err * (1 + e) + ds * (e + UB + 4 * U) + lost
             tol[0][b, h] += self.c * ((ds_err + ds * U * (M + 40)) @ np.abs(k))
-            tol[1][b, kv, at] += self.c * ((ds_err + ds * U * (N * group + 300)).T @ np.abs(q))
+            # dK may be formed with what delta is without out's rounding: the sum of P dP
+            off = np.abs((p * (go @ v.T)).sum(-1, keepdims=True) - (go * o64[b, h]).sum(-1, keepdims=True))
+            tol[1][b, kv, at] += self.c * ((ds_err + p * off + (ds + p * off) * U * (N * group + 300)).T @ np.abs(q))
             tol[2][b, kv, at] += (p * (e + UB + U * (N * group + 300)) + TINY).T @ np.abs(go)
         for name, a, w, t in zip(("dq", "dk", "dv"), got, want, tol):
             d = np.abs(a.double().cpu().numpy() - w)
