@@ -29,7 +29,7 @@ template <int D, int QT, bool MASK, bool LSE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, QT == 2 ? 2 : 4)))
 void cross_attn_kernel(CrossArgs a) {
   using G16 = Geo16<D>;
-  using Feed = KeyFeed<D, MASK>;
+  using Feed = KeyFeed<D, MASK, false>;
   constexpr int CT = TileLoader<D>::CT;
   __shared__ __attribute__((aligned(1024))) unsigned char Ks[NST][CT];
   __shared__ __attribute__((aligned(1024))) unsigned char Vs[NST][CT];

@@ -177,8 +177,20 @@ struct TileLoader {
       }
     }
   }
+  // the same by the near offsets, for masks with holes
+  __device__ __forceinline__ void load_some_near(const uint16_t* tile, const uint32_t (&off)[NUW], uint32_t bits, unsigned lds) const {
+    const uint32_t mine = bits >> row(0);
+#pragma unroll
+    for (int u = 0; u < NUW; ++u)
+      if (!PAD || piece(u) < G::DCH) {
+        const void* p = reinterpret_cast<const unsigned char*>(tile) + off[u];
+        global_to_lds<16>(mine >> (u * G::RPI) & 1 ? p : (const void*)kZeros, lds + (w * NUW + u) * 1024);
+      }
+  }
+  template <bool HOLES = false>
   __device__ __forceinline__ void load(const uint16_t* tile, int64_t pitch, const uint32_t (&off)[NUW], uint32_t bits, unsigned lds) const {
     if (__builtin_expect(bits == ~0u && near(pitch), 1)) load_near(tile, off, lds);
+    else if (HOLES && near(pitch)) load_some_near(tile, off, bits, lds);
     else load_some(tile, pitch, bits, lds);
   }
 };
@@ -255,8 +267,8 @@ struct Item {
 
 // Feeds tiles of K and V to a workgroup, over and over for one row tile after the other,
 // and says which of a tile's keys are seen: with a mask, a word of `bits` for each tile,
-// read a step ahead as a scalar.
-template <int D, bool MASK>
+// read a step ahead as a scalar.  KEYS_TOO: zeros in place of hidden rows of K as of V.
+template <int D, bool MASK, bool KEYS_TOO>
 struct KeyFeed {
   using Loader = TileLoader<D>;
   static constexpr int NUW = Loader::NUW;
@@ -295,8 +307,9 @@ struct KeyFeed {
   // the next tile into LDS, after the last one the first; returns which of its keys are seen
   __device__ __forceinline__ uint32_t feed(const CrossArgs& a, unsigned ks, unsigned vs) {
     const uint32_t now = __builtin_amdgcn_readfirstlane(word);
-    ld.load(kp, a.k.sn, koff, now, ks);
-    ld.load(vp, a.v.sn, voff, now, vs);
+    // hidden keys of a mask are read where their logits alone are formed (and replaced)
+    ld.template load<MASK && KEYS_TOO>(kp, a.k.sn, koff, MASK && !KEYS_TOO ? rows_left(left) : now, ks);
+    ld.template load<MASK>(vp, a.v.sn, voff, now, vs);
     kp += CK * a.k.sn;
     vp += CK * a.v.sn;
     left -= CK;
