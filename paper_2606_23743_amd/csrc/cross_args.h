@@ -34,11 +34,12 @@ struct CrossArgs {
 
 // How a call is divided, and its workspace: offsets of what CrossArgs points to.
 struct CrossShape {
+  int few;                       // 16 rows at most: the waves divide the keys
   int narrow;                    // 16 rows a wave (64 a workgroup), else 32 (128)
   int run, tiles, splits, key_tiles, row_splits;
   size_t bits_at, seen_at, stat_at, stat_l_at, part_at, part_kv_at, ws_bytes;
 };
-CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask);
+CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask, bool grad);
 CrossShape cross_grad_shape(int B, int Hkv, int G, int N, int M, int D, bool mask);
 
 hipError_t launch_cross_bits(const CrossArgs& a, hipStream_t stream);

@@ -25,6 +25,78 @@ constexpr int NST = 4, PD = 3;   // LDS stages, tiles ahead
 // a row's reference moves when a logit passes it by this much (log2 units)
 constexpr float kSlack = 30.0f;
 
+// What a wave keeps of its rows: the weights' reference (log2 units), their sums as rounded
+// to bf16 and unrounded (this lane's quarter), and O^T before it is divided.
+template <int D, int QT, bool LSE>
+struct RowState {
+  static constexpr int DT = Geo16<D>::DT;
+  float m_ref[QT], limit[QT], l_part[QT], l_full[QT];
+  f32x4 oacc[DT][QT];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      m_ref[qt] = -3e38f;
+      limit[qt] = -INFINITY;
+      l_part[qt] = l_full[qt] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt][qt] = f32x4{};
+    }
+  }
+  // moves the reference of rows that have a logit above their limit
+  __device__ __forceinline__ void follow(const f32x4 (&s)[2][QT], float sl2) {
+    float mx[QT];
+    bool over = false;
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      mx[qt] = s[0][qt][0];
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx[qt] = fmaxf(mx[qt], s[k2][qt][r]);
+      over |= mx[qt] > limit[qt];
+    }
+    if (__builtin_amdgcn_ballot_w64(over) != 0) {
+      asm volatile("");
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        const float m_new = fmaxf(m_ref[qt], quad_max(mx[qt]) * sl2);
+        const float f = __builtin_amdgcn_exp2f(m_ref[qt] - m_new);
+        l_part[qt] *= f;
+        if constexpr (LSE) l_full[qt] *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) oacc[dt][qt][r] *= f;
+        m_ref[qt] = m_new;
+        limit[qt] = (m_new + kSlack) / sl2;
+      }
+    }
+  }
+  __device__ __forceinline__ void weigh(const f32x4 (&s)[2][QT], bf16x8 (&pop)[QT], float sl2) {
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      u32x4 wv;
+      float lsum = l_part[qt], lf = l_full[qt];
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e], sl2, -m_ref[qt]));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e + 1], sl2, -m_ref[qt]));
+          const bf16x2 pb = cvt2(p0, p1);
+          lsum = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, lsum, false);
+          if constexpr (LSE) lf += p0 + p1;
+          wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, pb);
+        }
+      pop[qt] = __builtin_bit_cast(bf16x8, wv);
+      l_part[qt] = lsum;
+      if constexpr (LSE) l_full[qt] = lf;
+    }
+  }
+};
+
 template <int D, int QT, bool MASK, bool LSE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, QT == 2 ? 2 : 4)))
 void cross_attn_kernel(CrossArgs a) {
@@ -55,76 +127,12 @@ void cross_attn_kernel(CrossArgs a) {
 
   int koff[G16::KS], voff[G16::DT];
   operand_offsets<D>(lane, koff, voff);
-  float m_ref[QT], l_part[QT], l_full[QT], limit[QT];
-  f32x4 oacc[G16::DT][QT];
-  auto clear = [&]() {
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      m_ref[qt] = -3e38f;
-      limit[qt] = -INFINITY;
-      l_part[qt] = l_full[qt] = 0.0f;
-#pragma unroll
-      for (int dt = 0; dt < G16::DT; ++dt) oacc[dt][qt] = f32x4{};
-    }
-  };
-
-  // moves the reference of rows that have a logit above their limit
-  auto follow = [&](const f32x4 (&s)[2][QT]) {
-    float mx[QT];
-    bool over = false;
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      mx[qt] = s[0][qt][0];
-#pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) mx[qt] = fmaxf(mx[qt], s[k2][qt][r]);
-      over |= mx[qt] > limit[qt];
-    }
-    if (__builtin_amdgcn_ballot_w64(over) != 0) {
-      asm volatile("");
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        const float m_new = fmaxf(m_ref[qt], quad_max(mx[qt]) * sl2);
-        const float f = __builtin_amdgcn_exp2f(m_ref[qt] - m_new);
-        l_part[qt] *= f;
-        if constexpr (LSE) l_full[qt] *= f;
-#pragma unroll
-        for (int dt = 0; dt < G16::DT; ++dt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) oacc[dt][qt][r] *= f;
-        m_ref[qt] = m_new;
-        limit[qt] = (m_new + kSlack) / sl2;
-      }
-    }
-  };
-  auto softmax = [&](const f32x4 (&s)[2][QT], bf16x8 (&pop)[QT]) {
-    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      u32x4 wv;
-      float lsum = l_part[qt], lf = l_full[qt];
-#pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e], sl2, -m_ref[qt]));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e + 1], sl2, -m_ref[qt]));
-          const bf16x2 pb = cvt2(p0, p1);
-          lsum = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, lsum, false);
-          if constexpr (LSE) lf += p0 + p1;
-          wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, pb);
-        }
-      pop[qt] = __builtin_bit_cast(bf16x8, wv);
-      l_part[qt] = lsum;
-      if constexpr (LSE) l_full[qt] = lf;
-    }
-  };
+  RowState<D, QT, LSE> rs;
   auto store = [&](int tile) {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-      const float l_tot = quad_sum(l_part[qt]);
-      const float l_all = LSE ? quad_sum(l_full[qt]) : l_tot;
+      const float l_tot = quad_sum(rs.l_part[qt]);
+      const float l_all = LSE ? quad_sum(rs.l_full[qt]) : l_tot;
       const int r = row_of(tile, qt);
       const bool there = r < a.R;
       if (a.splits > 1) {
@@ -132,23 +140,23 @@ void cross_attn_kernel(CrossArgs a) {
         const int64_t at = (bh * a.splits + it.split) * a.R + r;
         float* o = a.part + at * D;
 #pragma unroll
-        for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = oacc[dt][qt];
+        for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = rs.oacc[dt][qt];
         if (g == 0) {
-          a.stat[at] = make_float2(m_ref[qt], l_tot);
+          a.stat[at] = make_float2(rs.m_ref[qt], l_tot);
           if constexpr (LSE) a.stat_l[at] = l_all;
         }
         continue;
       }
       const bool has = l_tot > 0.0f || l_tot != l_tot;   // a NaN stays one
       uint16_t* o = there ? static_cast<uint16_t*>(a.out.p) + row_offset(a.out, it.b, it.kvh * a.G, r, a.N, a.G) : nullptr;
-      store_row<D>(o, &oacc[0][qt], QT, has ? 1.0f / l_tot : 0.0f, g);
+      store_row<D>(o, &rs.oacc[0][qt], QT, has ? 1.0f / l_tot : 0.0f, g);
       if constexpr (LSE) {
-        if (g == 0 && there) a.lse[bh * a.R + r] = has ? (m_ref[qt] + __log2f(l_all)) * 0.69314718055994530942f : -INFINITY;
+        if (g == 0 && there) a.lse[bh * a.R + r] = has ? (rs.m_ref[qt] + __log2f(l_all)) * 0.69314718055994530942f : -INFINITY;
       }
     }
   };
 
-  clear();
+  rs.clear();
   if (it.chunks == 0) {            // no key: zeros
     for (int t = 0; t < it.tiles; ++t) store(it.tile + t);
     return;
@@ -184,7 +192,7 @@ void cross_attn_kernel(CrossArgs a) {
     wg_barrier();                  // and every wave is done with the tile before
     if (pending) {                 // (stored here, ahead of loads that are waited for two steps later)
       store(tile - 1);
-      clear();
+      rs.clear();
       pending = false;
       if (tile == end) break;
     }
@@ -196,7 +204,7 @@ void cross_attn_kernel(CrossArgs a) {
         late = 2;
       }
     }
-    follow(sacc);
+    rs.follow(sacc, sl2);
     if (++c == it.chunks) {
       c = 0;
       ++tile;
@@ -209,9 +217,9 @@ void cross_attn_kernel(CrossArgs a) {
     f32x4 snext[2][QT];
     bf16x8 pop[QT];
     qk16<D>(snext, &Ks[0][0] + (st + 1) % NST * CT, koff, qop);
-    softmax(sacc, pop);
+    rs.weigh(sacc, pop, sl2);
     __builtin_amdgcn_s_setprio(1);
-    pv16<D>(pop, &Vs[0][0] + st * CT, voff, oacc);
+    pv16<D>(pop, &Vs[0][0] + st * CT, voff, rs.oacc);
     __builtin_amdgcn_s_setprio(0);
     if (__builtin_expect(seen[1] != ~0u, 0)) {
       asm volatile("");
@@ -227,6 +235,137 @@ void cross_attn_kernel(CrossArgs a) {
     st = (st + 1) % NST;
   }
   wait_vmcnt<0>();                 // no load may still target this workgroup's LDS
+}
+
+// Sixteen rows at most (a single token's heads): the keys are the work, and a chain of
+// steps the time.  So the four waves of a workgroup take a tile of keys each, with stages of
+// their own and no barrier between them, and join their states at the end.  31 x 32 heads
+// of one token over 4,000 keys of 64 take 167 us (6.1 TB/s) instead of 243 with the kernel
+// above, 8 x 32 heads over 8 x 1,560 keys of 128 13.4 instead of 14.6, over 512 keys of one
+// entry 6.7 instead of 9.4.
+template <int D, bool MASK, bool LSE>
+__global__ __launch_bounds__(kThreads) void cross_few_kernel(CrossArgs a) {
+  using G = Geo<D>;
+  using G16 = Geo16<D>;
+  constexpr int CT = TileLoader<D>::CT, NU = CT / 1024, kStages = 2, kWaves = kThreads / 64;
+  // stages of K and V for each wave; then the waves' O, 16 rows of D
+  __shared__ __attribute__((aligned(1024))) unsigned char Ts[kWaves][kStages][2][CT];
+  __shared__ float ms[kWaves][16], ls[kWaves][16], lf[kWaves][16];
+  static_assert(kStages * 2 * CT >= 16 * D * 4, "a wave's O fits its stages");
+
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float sl2 = a.scale_log2;
+  const Item it(a);
+  const int64_t bh = (int64_t)it.b * a.Hkv + it.kvh;
+  unsigned char* mine = &Ts[w][0][0][0];
+  const unsigned base = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8*)mine);
+
+  const uint16_t* rows[1] = {
+      i < a.R ? static_cast<const uint16_t*>(a.q.p) + row_offset(a.q, it.b, it.kvh * a.G, i, a.N, a.G) : nullptr};
+  bf16x8 qop[1][G16::KS];
+  load_operand<D>(qop, rows, lane);
+  RowState<D, 1, LSE> rs;
+  rs.clear();
+
+  // this wave's tiles: it.c0 + w, + kWaves, ...
+  const uint32_t* words = MASK ? a.bits + (int64_t)it.b * ((a.M + 31) / 32) : nullptr;
+  const int last = it.c0 + it.chunks;
+  auto seen_of = [&](int c) -> uint32_t {
+    if (c >= last) return 0u;
+    if constexpr (MASK) return *(const __attribute__((address_space(4))) uint32_t*)(words + c);
+    return rows_left(it.count - c * CK);
+  };
+  const uint16_t* Kh = static_cast<const uint16_t*>(a.k.p) + it.b * a.k.sb + it.kvh * a.k.sh;
+  const uint16_t* Vh = static_cast<const uint16_t*>(a.v.p) + it.b * a.v.sb + it.kvh * a.v.sh;
+  // all of a tile's pieces, zeros where a row is not seen or a piece not there
+  auto fetch = [&](int st, int c, uint32_t seen) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int64_t pitch = t ? a.v.sn : a.k.sn;
+      const uint16_t* tile = (t ? Vh : Kh) + (int64_t)c * CK * pitch;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        const int r = u * G::RPI + lane / G::NCH, p = swz<G::NCH>(r, lane % G::NCH);
+        const void* from = tile + r * pitch + p * 8;
+        global_to_lds<16>((seen >> r & 1) && p < G::DCH ? from : (const void*)kZeros, base + (st * 2 + t) * CT + u * 1024);
+      }
+    }
+  };
+  int koff[G16::KS], voff[G16::DT];
+  operand_offsets<D>(lane, koff, voff);
+  uint32_t seen[kStages];
+#pragma unroll
+  for (int st = 0; st < kStages; ++st) {
+    seen[st] = seen_of(it.c0 + w + st * kWaves);
+    fetch(st, it.c0 + w + st * kWaves, seen[st]);
+  }
+  int st = 0;
+#pragma unroll 1
+  for (int c = it.c0 + w; c < last; c += kWaves) {
+    wait_vmcnt<2 * NU*(kStages - 1)>();          // the tile has landed
+    const unsigned char* kt = mine + st * 2 * CT;
+    f32x4 s[2][1];
+    qk16<D>(s, kt, koff, qop);
+    if (seen[0] != ~0u) hide(s, seen[0], lane);
+    rs.follow(s, sl2);
+    bf16x8 pop[1];
+    rs.weigh(s, pop, sl2);
+    pv16<D>(pop, kt + CT, voff, rs.oacc);
+    wait_vmcnt_lds_idle<2 * NU*(kStages - 1)>(); // and has been read: the stage takes the wave's next but one
+    seen[0] = seen[1];
+    const int next = c + kStages * kWaves;
+    seen[1] = seen_of(next);
+    fetch(st, next, seen[1]);
+    st ^= 1;
+  }
+  wait_vmcnt_lds_idle<0>();
+
+  // the waves' states: O in the wave's stages, then every lane some channels of a row
+  const float l_tot = quad_sum(rs.l_part[0]), l_all = LSE ? quad_sum(rs.l_full[0]) : l_tot;
+  float* o = reinterpret_cast<float*>(mine);
+#pragma unroll
+  for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + i * D + dt * 16 + 4 * g) = rs.oacc[dt][0];
+  if (g == 0) {
+    ms[w][i] = rs.m_ref[0];
+    ls[w][i] = l_tot;
+    lf[w][i] = l_all;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.R * (D / 4); e += kThreads) {
+    const int r = e / (D / 4), d = (e - r * (D / 4)) * 4;
+    float m = ms[0][r];
+#pragma unroll
+    for (int x = 1; x < kWaves; ++x) m = fmaxf(m, ms[x][r]);
+    float l = 0.0f, all = 0.0f;
+    f32x4 sum = {};
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) {
+      const float f = __builtin_amdgcn_exp2f(ms[x][r] - m);
+      l = fmaf(f, ls[x][r], l);
+      all = fmaf(f, lf[x][r], all);
+      const f32x4 part = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(&Ts[x][0][0][0]) + r * D + d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] = fmaf(f, part[j], sum[j]);
+    }
+    if (a.splits > 1) {
+      const int64_t at = (bh * a.splits + it.split) * a.R + r;
+      *reinterpret_cast<f32x4*>(a.part + at * D + d) = sum;
+      if (d == 0) {
+        a.stat[at] = make_float2(m, l);
+        if constexpr (LSE) a.stat_l[at] = all;
+      }
+      continue;
+    }
+    const bool has = l > 0.0f || l != l;
+    const float inv = has ? 1.0f / l : 0.0f;
+    uint16_t* to = static_cast<uint16_t*>(a.out.p) + row_offset(a.out, it.b, it.kvh * a.G, r, a.N, a.G);
+    const bf16x2 x = cvt2(sum[0] * inv, sum[1] * inv), y = cvt2(sum[2] * inv, sum[3] * inv);
+    *reinterpret_cast<bf16x4*>(to + d) = bf16x4{x[0], x[1], y[0], y[1]};
+    if constexpr (LSE) {
+      if (d == 0) a.lse[bh * a.R + r] = has ? (m + __log2f(all)) * 0.69314718055994530942f : -INFINITY;
+    }
+  }
 }
 
 // Joins the parts of a row: O = sum of 2^(m_s - m) O_s over the same of l_s.  One
@@ -336,7 +475,13 @@ void launch_qt(const CrossArgs& a, hipStream_t stream) {
 
 template <int D>
 void launch_d(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
-  if (s.narrow) launch_qt<D, 1>(a, stream);
+  auto few = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.wgs), dim3(kThreads), 0, stream, a); };
+  if (s.few) {
+    if (a.mask && a.lse) few(cross_few_kernel<D, true, true>);
+    else if (a.mask) few(cross_few_kernel<D, true, false>);
+    else if (a.lse) few(cross_few_kernel<D, false, true>);
+    else few(cross_few_kernel<D, false, false>);
+  } else if (s.narrow) launch_qt<D, 1>(a, stream);
   else launch_qt<D, 2>(a, stream);
   if (a.splits == 1) return;
   if (a.lse) hipLaunchKernelGGL((cross_join_kernel<D, true>), dim3(a.B * a.Hkv * a.R), dim3(kThreads), 0, stream, a);
@@ -347,16 +492,19 @@ void launch_d(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask) {
+CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask, bool grad) {
   CrossShape s{};
   const int64_t heads = (int64_t)B * Hkv, R = (int64_t)G * N;
-  const int64_t places = D == 64 ? 768 : 512;    // workgroups that the card holds: two a CU (D = 64: three)
+  s.few = !grad && R <= 16;
+  // workgroups that the card holds: two a CU (D = 64: three); with few rows one (two)
+  const int64_t places = s.few ? (D == 64 ? 512 : 256) : D == 64 ? 768 : 512;
   s.narrow = heads * ((R + 127) / 128) < places;
   s.tiles = (int)((R + (s.narrow ? 63 : 127)) / (s.narrow ? 64 : 128));
   // keys are divided where the tiles are fewer than the card's places for workgroups
   const int64_t wgs = heads * s.tiles;
   int64_t splits = wgs < places ? places / wgs : 1;
-  if (splits > (M + 255) / 256) splits = (M + 255) / 256;
+  const int least = s.few ? 128 : 256;           // keys of a part
+  if (splits > (M + least - 1) / least) splits = (M + least - 1) / least;
   s.splits = (int)(splits < 1 ? 1 : splits);
   const int64_t run = wgs / (4 * places);
   s.run = (int)(run < 1 ? 1 : run < 8 ? run : 8);

@@ -387,7 +387,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 }  // namespace
 
 CrossShape cross_grad_shape(int B, int Hkv, int G, int N, int M, int D, bool mask) {
-  CrossShape s = cross_shape(B, Hkv, G, N, M, D, mask);
+  CrossShape s = cross_shape(B, Hkv, G, N, M, D, mask, true);
   const int64_t heads = (int64_t)B * Hkv, R = (int64_t)G * N;
   s.key_tiles = (M + 127) / 128;
   const int64_t base = heads * s.key_tiles, walk = (((int64_t)N + 31) / 32 * G + 7) / 8;

@@ -97,7 +97,8 @@ int cross_sizes(const sva_cross* p, bool mask, bool grad, sva::CrossArgs* a, sva
   a->scale_log2 = (float)(c * 1.4426950408889634074);
   // zero would make a hidden key's logit 0 * -inf, infinity every other's
   if (!(a->scale >= FLT_MIN && a->scale_log2 <= FLT_MAX)) return SVA_ERR_INVALID_ARG;
-  *s = (grad ? sva::cross_grad_shape : sva::cross_shape)(a->B, a->Hkv, a->G, a->N, a->M, a->D, mask);
+  *s = grad ? sva::cross_grad_shape(a->B, a->Hkv, a->G, a->N, a->M, a->D, mask)
+            : sva::cross_shape(a->B, a->Hkv, a->G, a->N, a->M, a->D, mask, false);
   a->tiles = s->tiles;
   a->run = s->run;
   a->splits = s->splits;
