@@ -14,8 +14,8 @@ from ._lib import (SvaError, Problem, SelectParams, RopeParams, load, problem, p
                    quantize_fp8, sparse_attention_fp8, dense_attention_fp8, remainder_workspace,
                    block_moments, sparse_attention_remainder, rotary_frequencies, rotary_plan, rotary, kv_cache,
                    cache_write, cache_read, cache_attention_workspace, cache_attention)
-from ._layer import (rotary_axes_plan, rotary_axes, layer_norm, layer_norm_backward_workspace, layer_norm_backward, cross_attention_workspace,
-                     cross_attention, cross_attention_backward)
+from ._layer import (rotary_axes_plan, rotary_axes, layer_norm, layer_norm_backward_workspace, layer_norm_backward,
+                     cross_attention_workspace, cross_attention, cross_attention_backward)
 
 __all__ = [
     "workloads", "SvaError", "Problem", "SelectParams", "RopeParams", "load", "problem",

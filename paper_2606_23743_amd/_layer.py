@@ -93,28 +93,39 @@ def _rows(t, dtype, shape, name, dev) -> Rows:
     return Rows(t.data_ptr(), sb, sn)
 
 
+def _norm_rows(t, B, C, name, dev):
+    """weight or bias, [C] or [B, C]: 1 for a row per entry, and the stride of entries."""
+    if not (isinstance(t, _torch().Tensor) and t.get_device() == dev):
+        _on_device(t, name)
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2 and shape[0] == B and shape[1] == C:
+        per, stride = 1, strides[0]
+    elif len(shape) == 1 and shape[0] == C:
+        per = stride = 0
+    else:
+        raise ValueError(f"{name} must have shape {(C,)} or {(B, C)}, got {tuple(shape)}")
+    if C > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}'s channels must be contiguous")
+    return per, stride
+
+
 def _norm_weights(weight, bias, B, C, dev):
     """weight and bias, [C] or [B, C] and of one type: (pointers, type code, per entry, strides)."""
-    torch = _torch()
-    both = [t for t in (weight, bias) if t is not None]
-    for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is None:
-            continue
-        _on_device(t, name)
-        if t.shape != (C,) and t.shape != (B, C):
-            raise ValueError(f"{name} must have shape {(C,)} or {(B, C)}, got {tuple(t.shape)}")
-        if C > 1 and t.stride(-1) != 1:
-            raise ValueError(f"{name}'s channels must be contiguous")
-    if len(both) == 2 and both[0].dtype != both[1].dtype:
-        raise TypeError(f"weight and bias must have one type, got {both[0].dtype} and {both[1].dtype}")
-    if len(both) == 2 and both[0].dim() != both[1].dim():
-        raise ValueError("weight and bias must both be [C] or both [B, C]")
-    if not both:
+    if weight is None and bias is None:
         return None, None, SVA_F32, 0, 0, 0
-    _, code = _dtype_code(both[0].dtype, "weight and bias")
-    per = both[0].dim() == 2
-    return (_ptr(weight), _ptr(bias), code, 1 if per else 0, weight.stride(0) if per and weight is not None else 0,
-            bias.stride(0) if per and bias is not None else 0)
+    per_w = per_b = None
+    w_s = b_s = 0
+    if weight is not None:
+        per_w, w_s = _norm_rows(weight, B, C, "weight", dev)
+    if bias is not None:
+        per_b, b_s = _norm_rows(bias, B, C, "bias", dev)
+    if weight is not None and bias is not None:
+        if weight.dtype != bias.dtype:
+            raise TypeError(f"weight and bias must have one type, got {weight.dtype} and {bias.dtype}")
+        if per_w != per_b:
+            raise ValueError("weight and bias must both be [C] or both [B, C]")
+    _, code = _dtype_code((bias if weight is None else weight).dtype, "weight and bias")
+    return _ptr(weight), _ptr(bias), code, per_b if weight is None else per_w, w_s, b_s
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, unit_offset: bool = False, y=None, want_stats: bool = False,
@@ -144,7 +155,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, unit_offset: bool =
     prm = LayerNormParams(B, N, C, code, w_code, per, 1 if unit_offset else 0, w_s, b_s, float(eps))
     _check(_lib.load().sva_layer_norm(prm, rx, w, b, _rows(y, dt, shp, "y", dev), mp, rp, _stream_on(stream, dev)),
            "sva_layer_norm")
-    _record(stream, x, weight, bias, y, mean, rstd)
+    if stream is not None:
+        _record(stream, x, weight, bias, y, mean, rstd)
     return y, mean, rstd
 
 
@@ -154,6 +166,9 @@ def layer_norm_backward_workspace(batch: int, n_tokens: int, channels: int, per_
     prm = LayerNormParams(batch, n_tokens, channels, SVA_BF16, SVA_F32, 1 if per_entry else 0, 0, 0, 0, 1.0)
     _check(_lib.load().sva_layer_norm_backward_workspace(prm, ctypes.byref(out)), "sva_layer_norm_backward_workspace")
     return out.value
+
+
+_norm_bytes = {}           # workspace bytes by sizes
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, unit_offset: bool = False, dx=None, want_weight: bool = True,
@@ -190,7 +205,11 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, unit_offset: bool = Fals
         ws_bytes = workspace.numel()
         ws_ptr = _plain(workspace, torch.uint8, (ws_bytes,), "workspace", dev)
     elif dweight is not None or dbias is not None:
-        ws_bytes = layer_norm_backward_workspace(B, N, C, bool(per))
+        ws_bytes = _norm_bytes.get((B, N, C, per))
+        if ws_bytes is None:
+            if len(_norm_bytes) > 4096:
+                _norm_bytes.clear()
+            ws_bytes = _norm_bytes[B, N, C, per] = layer_norm_backward_workspace(B, N, C, bool(per))
         if ws_bytes:
             workspace = _scratch(stream, ws_bytes, x.device)
             ws_ptr = workspace.data_ptr()
@@ -200,7 +219,8 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, unit_offset: bool = Fals
         None if dweight is None else _plain(dweight, torch.float32, sums, "dweight", dev),
         None if dbias is None else _plain(dbias, torch.float32, sums, "dbias", dev), _stream_on(stream, dev)),
         "sva_layer_norm_backward")
-    _record(stream, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace)
+    if stream is not None:
+        _record(stream, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace)
     return dx, dweight, dbias
 
 
@@ -282,7 +302,8 @@ def cross_attention(q, k, v, lengths=None, mask=None, softmax_scale: float = 0.0
     workspace, ws_ptr, ws_bytes = _cross_workspace(workspace, stream, (prm, mk is not None, q.device), dev, False)
     _check(_lib.load().sva_cross_attention(prm, hq, hk, hv, lens, mk, mask_b, ws_ptr, ws_bytes, ho, lp, _stream_on(stream, dev)),
            "sva_cross_attention")
-    _record(stream, q, k, v, lengths, mask, workspace, out, lse)
+    if stream is not None:
+        _record(stream, q, k, v, lengths, mask, workspace, out, lse)
     return out, lse
 
 
@@ -306,5 +327,6 @@ def cross_attention_backward(dout, q, k, v, out, lse, lengths=None, mask=None, s
     workspace, ws_ptr, ws_bytes = _cross_workspace(workspace, stream, (prm, mk is not None, q.device), dev, True)
     _check(_lib.load().sva_cross_attention_backward(prm, hg, hq, hk, hv, ho, lp, lens, mk, mask_b, ws_ptr, ws_bytes, gq, gk, gv,
                                                _stream_on(stream, dev)), "sva_cross_attention_backward")
-    _record(stream, dout, q, k, v, out, lse, lengths, mask, workspace, dq, dk, dv)
+    if stream is not None:
+        _record(stream, dout, q, k, v, out, lse, lengths, mask, workspace, dq, dk, dv)
     return dq, dk, dv

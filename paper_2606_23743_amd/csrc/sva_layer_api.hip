@@ -108,6 +108,7 @@ int cross_sizes(const sva_cross* p, bool mask, bool grad, sva::CrossArgs* a, sva
   const int64_t heads = (int64_t)a->B * a->Hkv, most = ((int64_t)1 << 24) - 1;
   const int64_t wgs = heads * ((s->tiles + s->run - 1) / s->run) * s->splits, kv_wgs = heads * s->key_tiles * s->row_splits;
   if (wgs > most || kv_wgs > most || (s->splits > 1 && heads * a->R > most)) return SVA_ERR_SHAPE;
+  if (mask && a->B > most / 4) return SVA_ERR_SHAPE;      // (an entry's mask: 1,024 threads)
   a->wgs = (int)wgs;
   a->kv_wgs = (int)kv_wgs;
   return SVA_OK;

@@ -175,6 +175,8 @@ def test_cross_attention_refusals(lib):
                    dict(lse=A + 2), dict(ws=A + 128)):
             assert f(**kw) == ALIGN, kw
         assert f(head_dim=80) == UNSUP and f(head_dim=256) == UNSUP
+        assert f(batch=1 << 23, heads=1, kv_heads=1, queries=1, keys=1) == SHAPE    # more masks than a launch takes
+        assert f(batch=1 << 25, heads=1, kv_heads=1, queries=1, keys=1, mask=None) == SHAPE
     for t in (q, k, v):
         assert fwd(out=Heads(t.data, 4, 4 * N * D, N * D, D)) == BAD
     assert fwd(out=Heads(A + 3 * MB, 4, 4 * N * D, 0, D)) == BAD            # an output that repeats itself
