@@ -53,28 +53,8 @@ struct Places {
   }
 };
 
-// S = rows of the tile at LDS address `tile` times the rows in registers: for the tile's
-// rows 16x + 4g + r and the register rows 16qt + i, sum over d
-template <int D, int QT>
-__device__ __forceinline__ void rows_times(f32x4 (&s)[2][QT], unsigned tile, const Places<D>& at,
-                                           const bf16x8 (&op)[QT][Geo16<D>::KS]) {
-  using G = Geo<D>;
-  const unsigned p = tile + at.row;
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) s[x][qt] = f32x4{};
-#pragma unroll
-  for (int k = 0; k < Geo16<D>::KS; ++k)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const bf16x8 row = *(lds_bf16x8*)(size_t)((p ^ (k << 6)) + x * 16 * G::RB);
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) s[x][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, op[qt][k], s[x][qt], 0, 0, 0);
-    }
-}
-
-// 16 of a tile's rows times those in registers
+// S = 16 of a tile's rows, the first at LDS address `tile`, times the rows in registers:
+// for the tile's rows 4g + r and the register rows 16qt + i, sum over d
 template <int D, int QT>
 __device__ __forceinline__ void rows_times_half(f32x4 (&s)[QT], unsigned tile, const Places<D>& at,
                                                 const bf16x8 (&op)[QT][Geo16<D>::KS]) {
