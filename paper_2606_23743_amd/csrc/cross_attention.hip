@@ -97,11 +97,6 @@ struct RowState {
   }
 };
 
-// Workgroups of 32 rows a wave that a CU holds: two, whose waves have 256 registers each.
-// Heads of 64 fit the 168 of three: 31,620 tokens' 40 heads over 512 keys take 260 us
-// instead of 305.
-constexpr int wide_per_cu(int D) { return D == 64 ? 3 : 2; }
-
 template <int D, int QT, bool MASK, bool LSE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(wide_per_cu(D), QT == 2 ? wide_per_cu(D) : 4)))
 void cross_attn_kernel(CrossArgs a) {
@@ -373,18 +368,21 @@ __global__ __launch_bounds__(kThreads) void cross_few_kernel(CrossArgs a) {
   }
 }
 
-// Joins the parts of a row: O = sum of 2^(m_s - m) O_s over the same of l_s.  One
-// workgroup a row, its waves a run of parts each, then those in order.
-template <int D, bool LSE>
+// Joins the parts of a row: O = sum of 2^(m_s - m) O_s over the same of l_s.  W waves a
+// row, a run of parts each, then those in order.
+template <int D, bool LSE, int W>
 __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
   __shared__ float os[4][128], ls[4], lf[4], ms[4];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int bh = blockIdx.x / a.R, r = blockIdx.x - bh * a.R;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, x0 = w % W;
+  const int64_t row = (int64_t)blockIdx.x * (4 / W) + w / W;
+  if (row >= (int64_t)a.B * a.Hkv * a.R) return;       // (W = 1 only: no barrier follows)
+  const int bh = (int)(row / a.R), r = (int)(row - (int64_t)bh * a.R);
   const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
-  const int s0 = a.splits * w / 4, s1 = a.splits * (w + 1) / 4;
+  const int s0 = a.splits * x0 / W, s1 = a.splits * (x0 + 1) / W;
   const int64_t at = (int64_t)bh * a.splits * a.R + r;
 
   float m = -3e38f;
+#pragma unroll 4
   for (int s = s0; s < s1; ++s) m = fmaxf(m, a.stat[at + (int64_t)s * a.R].x);
   float l = 0.0f, lall = 0.0f, o0 = 0.0f, o1 = 0.0f;
 #pragma unroll 4
@@ -400,24 +398,28 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
       o1 = fmaf(f, o.y, o1);
     }
   }
-  os[w][2 * lane] = o0;
-  os[w][2 * lane + 1] = o1;
-  if (lane == 0) {
-    ls[w] = l;
-    lf[w] = lall;
-    ms[w] = m;
-  }
-  __syncthreads();
-  if (w != 0) return;
-  const float top = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-  l = lall = o0 = o1 = 0.0f;
+  if constexpr (W > 1) {
+    os[w][2 * lane] = o0;
+    os[w][2 * lane + 1] = o1;
+    if (lane == 0) {
+      ls[w] = l;
+      lf[w] = lall;
+      ms[w] = m;
+    }
+    __syncthreads();
+    if (w != 0) return;
+    m = ms[0];
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    const float f = __builtin_amdgcn_exp2f(ms[x] - top);
-    l = fmaf(f, ls[x], l);
-    lall = fmaf(f, lf[x], lall);
-    o0 = fmaf(f, os[x][2 * lane], o0);
-    o1 = fmaf(f, os[x][2 * lane + 1], o1);
+    for (int x = 1; x < W; ++x) m = fmaxf(m, ms[x]);
+    l = lall = o0 = o1 = 0.0f;
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      const float f = __builtin_amdgcn_exp2f(ms[x] - m);
+      l = fmaf(f, ls[x], l);
+      lall = fmaf(f, lf[x], lall);
+      o0 = fmaf(f, os[x][2 * lane], o0);
+      o1 = fmaf(f, os[x][2 * lane + 1], o1);
+    }
   }
   const bool has = l > 0.0f || l != l;
   const float inv = has ? 1.0f / l : 0.0f;
@@ -427,9 +429,11 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
   }
   if constexpr (LSE) {
     if (lane == 0)
-      a.lse[((int64_t)b * a.H + kvh * a.G) * a.N + r] = has ? (top + __log2f(lall)) * 0.69314718055994530942f : -INFINITY;
+      a.lse[((int64_t)b * a.H + kvh * a.G) * a.N + r] = has ? (m + __log2f(lall)) * 0.69314718055994530942f : -INFINITY;
   }
 }
+
+constexpr int kWaveParts = 8;    // parts that one wave joins
 
 // An entry's mask and length as bits, a word for each tile of 32 keys, and its keys up to
 // the last seen one.  One workgroup an entry, a word a lane at a time.
@@ -489,28 +493,75 @@ void launch_d(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
   } else if (s.narrow) launch_qt<D, 1>(a, stream);
   else launch_qt<D, 2>(a, stream);
   if (a.splits == 1) return;
-  if (a.lse) hipLaunchKernelGGL((cross_join_kernel<D, true>), dim3(a.B * a.Hkv * a.R), dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((cross_join_kernel<D, false>), dim3(a.B * a.Hkv * a.R), dim3(kThreads), 0, stream, a);
+  auto join = [&](auto kernel, int waves) {
+    const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows * waves + 3) / 4)), dim3(kThreads), 0, stream, a);
+  };
+  if (a.splits > kWaveParts) {
+    if (a.lse) join(cross_join_kernel<D, true, 4>, 4);
+    else join(cross_join_kernel<D, false, 4>, 4);
+  } else {
+    if (a.lse) join(cross_join_kernel<D, true, 1>, 1);
+    else join(cross_join_kernel<D, false, 1>, 1);
+  }
 }
 
 }  // namespace
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Expected microseconds of a call with row tiles of 64 (narrow) or 128 and its keys divided
+// into parts.  A step over 32 keys takes a lone workgroup of a CU 0.85 us (narrow: 0.66) and
+// several 0.55 (0.43) each, 0.66 and 0.38 (0.51 and 0.30) with heads of 64; what parts add is
+// a launch and their results written and read.  Fitted to 240 calls of 32 to 32,768 rows over
+// 64 to 16,384 keys with every shape and up to 32 parts: the shape with the least cost takes
+// 1.01 times the best one's time in the geometric mean and 1.16 times at most.  Parts that
+// fill the card at any cost took 1.10 and 1.87 times: 32 heads of 512 rows over 512 keys
+// 28.5 us instead of 16, over 4,000 keys in narrow tiles 76.5 instead of 55 in wide ones.
+static float shape_cost(bool narrow, int64_t wgs, int64_t rows, int M, int D, int splits) {
+  const float lone = D == 64 ? (narrow ? 0.51f : 0.66f) : narrow ? 0.66f : 0.85f;
+  const float each = D == 64 ? (narrow ? 0.30f : 0.38f) : narrow ? 0.43f : 0.55f;
+  const int64_t per_cu = (wgs * splits + 255) / 256, steps = ((M + 31) / 32 + splits - 1) / splits;
+  float us = (float)steps * fmaxf(lone, (float)per_cu * each);
+  if (splits > 1) us += 3.3f + (float)rows * (float)(splits * D) * 8.0f / 3.6e6f;
+  return us;
+}
+
 CrossShape cross_shape(int B, int Hkv, int G, int N, int M, int D, bool mask, bool grad) {
   CrossShape s{};
   const int64_t heads = (int64_t)B * Hkv, R = (int64_t)G * N;
   s.few = !grad && R <= 16;
-  // workgroups that the card holds: two a CU (D = 64: three); with few rows one (two)
-  const int64_t places = s.few ? (D == 64 ? 512 : 256) : D == 64 ? 768 : 512;
-  s.narrow = heads * ((R + 127) / 128) < places;
-  s.tiles = (int)((R + (s.narrow ? 63 : 127)) / (s.narrow ? 64 : 128));
-  // keys are divided where the tiles are fewer than the card's places for workgroups
-  const int64_t wgs = heads * s.tiles;
-  int64_t splits = wgs < places ? places / wgs : 1;
-  const int least = s.few ? 128 : 256;           // keys of a part
-  if (splits > (M + least - 1) / least) splits = (M + least - 1) / least;
-  s.splits = (int)(splits < 1 ? 1 : splits);
+  s.splits = 1;
+  int64_t wgs = heads, places = wide_per_cu(D) * 256;   // workgroups; those that the card holds
+  if (s.few) {
+    // A single token's keys fill the card once (31 x 32 heads of 4,000 keys: 170 us, parts for
+    // twice or three times as many workgroups 195 and 211), in parts of 128 keys or more, a
+    // tile a wave.  Up to 512 keys (64 channels: 1,024) are read sooner than parts are
+    // joined: 4 x 20 heads of 64 over 512 keys take 6.4 us, in 6 parts 10.9.
+    s.narrow = s.tiles = 1;
+    if ((int64_t)M * D > 65536 && wgs < 256) {
+      const int64_t parts = 256 / wgs, most = (M + 127) / 128;
+      s.splits = (int)(parts < most ? parts : most);
+    }
+  } else {
+    float best = INFINITY;
+    for (int narrow = 0; narrow < 2; ++narrow) {
+      const int64_t tiles = (R + (narrow ? 63 : 127)) / (narrow ? 64 : 128);
+      for (int splits = 1; splits <= 64; splits += splits < 4 ? 1 : splits & (splits - 1) ? splits / 3 : splits / 2) {
+        if (splits > 1 && (heads * tiles * splits > places || M < 64 * splits)) break;
+        const float us = shape_cost(narrow, heads * tiles, heads * R, M, D, splits);
+        if (us >= best) continue;
+        best = us;
+        s.narrow = narrow;
+        s.tiles = (int)tiles;
+        s.splits = splits;
+      }
+    }
+    wgs = heads * s.tiles;
+  }
+  // Runs of row tiles, for which K and V are found and Q comes ahead, where the card is filled
+  // four times over: 63,240 rows of 32 heads over 512 keys 680 us, in runs of up to 16 and two
+  // rounds 796.
   const int64_t run = wgs / (4 * places);
   s.run = (int)(run < 1 ? 1 : run < 8 ? run : 8);
   size_t at = 0;

@@ -25,7 +25,7 @@ using namespace cross;
 constexpr int NST = 4, PD = 3;   // LDS stages, tiles ahead
 
 template <int D, int QT, bool MASK>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, QT == 2 ? 2 : 4)))
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(wide_per_cu(D), QT == 2 ? wide_per_cu(D) : 4)))
 void cross_grad_rows_kernel(CrossArgs a) {
   using G16 = Geo16<D>;
   using Feed = KeyFeed<D, MASK, true>;
@@ -391,9 +391,23 @@ CrossShape cross_grad_shape(int B, int Hkv, int G, int N, int M, int D, bool mas
   const int64_t heads = (int64_t)B * Hkv, R = (int64_t)G * N;
   s.key_tiles = (M + 127) / 128;
   const int64_t base = heads * s.key_tiles, walk = (((int64_t)N + 31) / 32 * G + 7) / 8;
-  int64_t parts = base < 1024 ? 1024 / base : 1;
-  if (parts > walk) parts = walk;
-  s.row_splits = (int)parts;
+  // The rows of a tile of keys are divided where that is worth its partial sums: a step over
+  // 32 rows takes a lone workgroup of a CU 1.56 us and a pair 1.95 (0.78 and 1.0 with heads of
+  // 64), parts a launch and their sums written and read.  Of 139 calls (1 to 16,384 rows, 64
+  // to 4,000 keys) timed with every number of parts, the one chosen took 1.003 times the best
+  // one's time in the geometric mean, 1.12 at most; parts for 1,024 workgroups 1.03 and 1.34
+  // (32 heads of 512 rows over 1,536 keys: 130 us instead of 96).
+  const float lone = D == 64 ? 0.78f : 1.56f, pair = D == 64 ? 1.0f : 1.95f;
+  float best = INFINITY;
+  for (int parts = 1; parts <= 1024; parts += parts < 4 ? 1 : parts & (parts - 1) ? parts / 3 : parts / 2) {
+    if (parts > 1 && (parts > walk || base * parts > 1024)) break;
+    const int64_t per_cu = (base * parts + 255) / 256, steps = (((int64_t)N + 31) / 32 * G + parts - 1) / parts;
+    float us = (float)steps * ((float)(per_cu / 2) * pair + (float)(per_cu % 2) * lone);
+    if (parts > 1) us += 3.3f + (float)(heads * M) * (float)(parts * D) * 16.0f / 3.6e6f;
+    if (us >= best) continue;
+    best = us;
+    s.row_splits = parts;
+  }
   size_t at = mask ? s.seen_at + up256((size_t)B * 4) : 0;
   s.stat_at = at;
   at += up256((size_t)heads * R * 8);

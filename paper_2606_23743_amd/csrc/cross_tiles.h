@@ -38,6 +38,11 @@ __device__ __forceinline__ void operand_offsets(int lane, int (&koff)[Geo16<D>::
 
 typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
+// Workgroups of 32 rows a wave that a CU holds: two, whose waves have 256 registers each.
+// Heads of 64 fit the 168 of three: 31,620 tokens' 40 heads over 512 keys take 260 us
+// instead of 305, with gradients another 819 instead of 850.
+constexpr int wide_per_cu(int D) { return D == 64 ? 3 : 2; }
+
 // A lane's place in a tile, for the row operands (row i at channels 8g .. +8) and for the
 // transpose reads (rows 4g.. at channels 0..).  Step s of the rows is at place ^ s << 6,
 // d tile dt at place ^ dt << 5, 16 rows further the swizzle is the same: one register
