@@ -6,9 +6,13 @@
 // bits; S and dP are formed in both (seven products where five would do, against
 // partial dQ of every key tile through memory).
 //   rows: a workgroup holds 128 (64) rows, as the forward kernel does, with Q and dO
-//     in registers, and walks the keys; P and dS stay in registers and are the operand
-//     of dQ^T += K^T dS^T as they stand.  It also forms delta, which the second launch
-//     reads.
+//     in registers, and walks the keys; P and dS stay in registers and are the operands
+//     of dQ^T += K^T dS^T and of (P K)^T as they stand.  It forms delta from out, which
+//     was rounded to bf16: what the dS of a row then sum to instead of zero, e, is given
+//     back, as dQ = c (dS K - e P K), and to the second launch as delta + e.  Without it
+//     dQ and dK of rows with one large weight were off by up to three times what their
+//     own rounding takes; P K costs an eighth of the call (63,240 rows of 32 heads over
+//     512 keys 2,305 us instead of 2,060), O formed again in place of e more.
 //   keys: a workgroup holds 128 keys (32 a wave) with K and V in registers and walks
 //     the rows of all heads of the group, so dK and dV are summed over them where they
 //     are; S = Q K^T here has the rows in the registers and a key in every lane, P and
@@ -43,30 +47,35 @@ void cross_grad_rows_kernel(CrossArgs a) {
   const int64_t bh = (int64_t)it.b * a.Hkv + it.kvh;
   auto row_of = [&](int tile, int qt) { return tile * 64 * QT + (w * QT + qt) * 16 + i; };
 
-  // Q and dO of the wave's rows, their lse and delta
+  // Q and dO of the wave's rows, their lse and delta.  (Loads of the next rows' during a
+  // tile's last product would keep 32 to 96 more registers alive beside both sums: 63,240
+  // rows over 512 keys 2,670 and 3,190 us instead of 2,305.)
   bf16x8 qop[QT][G16::KS], gop[QT][G16::KS];
   float lse2[QT], delta[QT], excess[QT];
   bf16x8 oop[QT][G16::KS];
   float lse[QT];
-  auto load_rows = [&](int tile) {
-    const uint16_t *qrow[QT], *grow[QT], *orow[QT];
+  auto take_rows = [&](int tile) {
+    const uint16_t *qrow[QT], *grow[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       const int r = row_of(tile, qt);
-      qrow[qt] = grow[qt] = orow[qt] = nullptr;
+      qrow[qt] = grow[qt] = nullptr;
       lse[qt] = -INFINITY;
       if (r < a.R) {
         qrow[qt] = static_cast<const uint16_t*>(a.q.p) + row_offset(a.q, it.b, it.kvh * a.G, r, a.N, a.G);
         grow[qt] = static_cast<const uint16_t*>(a.dout.p) + row_offset(a.dout, it.b, it.kvh * a.G, r, a.N, a.G);
-        orow[qt] = static_cast<const uint16_t*>(a.out.p) + row_offset(a.out, it.b, it.kvh * a.G, r, a.N, a.G);
         lse[qt] = a.lse[bh * a.R + r];
       }
     }
     load_operand<D>(qop, qrow, lane);
     load_operand<D>(gop, grow, lane);
+    const uint16_t* orow[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      const int r = row_of(tile, qt);
+      orow[qt] = r < a.R ? static_cast<const uint16_t*>(a.out.p) + row_offset(a.out, it.b, it.kvh * a.G, r, a.N, a.G) : nullptr;
+    }
     load_operand<D>(oop, orow, lane);
-  };
-  auto take_rows = [&]() {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       float s = 0.0f;
@@ -80,39 +89,45 @@ void cross_grad_rows_kernel(CrossArgs a) {
       excess[qt] = 0.0f;
     }
   };
-  // A row's dS sum to zero; what they sum to, here, is what out's rounding to bf16 took from
-  // delta, and the second launch gets delta with it.  (dQ has been summed with the other.)
-  auto put_stat = [&](int tile) {
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      const float d = a.splits == 1 ? delta[qt] + quad_sum(excess[qt]) : delta[qt];
-      const int r = row_of(tile, qt);
-      if (it.split == 0 && g == 0 && r < a.R) a.stat[bh * a.R + r] = make_float2(lse2[qt], d);
-    }
-  };
-  f32x4 dq[G16::DT][QT] = {};
+  // A row's dS sum to zero but for e, what out's rounding to bf16 took from delta: e is given
+  // back to delta for the second launch, and dQ is dS K - e P K.
+  f32x4 dq[G16::DT][QT] = {}, pk[G16::DT][QT] = {};
   auto store = [&](int tile) {
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       const int r = row_of(tile, qt);
-      if (r < a.R && a.splits > 1) {
-        float* o = a.part + ((bh * a.splits + it.split) * a.R + r) * D;
+      const float e = quad_sum(excess[qt]);
+      if (a.splits > 1) {
+        if (r < a.R) {
+          const int64_t at = (bh * a.splits + it.split) * a.R + r;
+          float* o = a.part + at * (2 * D);
 #pragma unroll
-        for (int dt = 0; dt < G16::DT; ++dt) *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = dq[dt][qt];
-      } else if (a.splits == 1) {
+          for (int dt = 0; dt < G16::DT; ++dt) {
+            *reinterpret_cast<f32x4*>(o + dt * 16 + 4 * g) = dq[dt][qt];
+            *reinterpret_cast<f32x4*>(o + D + dt * 16 + 4 * g) = pk[dt][qt];
+          }
+          if (g == 0) {
+            a.stat_l[at] = e;
+            if (it.split == 0) a.stat[bh * a.R + r] = make_float2(lse2[qt], delta[qt]);
+          }
+        }
+      } else {
         uint16_t* o = r < a.R ? static_cast<uint16_t*>(a.dq.p) + row_offset(a.dq, it.b, it.kvh * a.G, r, a.N, a.G) : nullptr;
+#pragma unroll
+        for (int dt = 0; dt < G16::DT; ++dt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dq[dt][qt][j] = fmaf(-e, pk[dt][qt][j], dq[dt][qt][j]);
         store_row<D>(o, &dq[0][qt], QT, a.scale, g);
+        if (g == 0 && r < a.R) a.stat[bh * a.R + r] = make_float2(lse2[qt], delta[qt] + e);
       }
 #pragma unroll
-      for (int dt = 0; dt < G16::DT; ++dt) dq[dt][qt] = f32x4{};
+      for (int dt = 0; dt < G16::DT; ++dt) dq[dt][qt] = pk[dt][qt] = f32x4{};
     }
   };
 
   if (it.chunks == 0) {            // no key: zeros
     for (int t = 0; t < it.tiles; ++t) {
-      load_rows(it.tile + t);
-      take_rows();
-      put_stat(it.tile + t);       // (other parts may have keys)
+      take_rows(it.tile + t);      // (other parts may have keys)
       store(it.tile + t);
     }
     return;
@@ -125,11 +140,9 @@ void cross_grad_rows_kernel(CrossArgs a) {
   uint32_t seen[PD];               // which keys of the tiles ahead are
 #pragma unroll
   for (int c = 0; c < PD; ++c) seen[c] = fetch(c);
-  load_rows(it.tile);
-  take_rows();
+  take_rows(it.tile);
 
-  int koff[G16::KS], voff[G16::DT];
-  operand_offsets<D>(lane, koff, voff);
+  const Places<D> at(lane);
   int st = 0, c = 0, tile = it.tile;
   const int end = it.tile + it.tiles;
 #pragma unroll 1
@@ -137,47 +150,52 @@ void cross_grad_rows_kernel(CrossArgs a) {
     wait_vmcnt_lds_idle<Feed::kLoads * (PD - 1)>();    // the tile has landed
     wg_barrier();                                      // and every wave is done with the one before
     const uint32_t fed = fetch((st + PD) % NST);
-    const unsigned char *kt = &Ks[0][0] + st * CT, *vt = &Vs[0][0] + st * CT;
-    f32x4 s[2][QT], dp[2][QT];
-    qk16<D>(s, kt, koff, qop);
-    qk16<D>(dp, vt, koff, gop);
-    if (__builtin_expect(seen[0] != ~0u, 0)) {
-      asm volatile("");
-      hide(s, seen[0], lane);
+    const unsigned kt = ks_base + st * CT, vt = vs_base + st * CT;
+    u32x4 pw[QT], dsw[QT];
+    // 16 keys at a time: 16 registers of S and dP are alive beside dQ and P K, not 32
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      f32x4 s[QT], dp[QT];
+      rows_times_half<D, QT>(s, kt + x * 16 * Geo<D>::RB, at, qop);
+      rows_times_half<D, QT>(dp, vt + x * 16 * Geo<D>::RB, at, gop);
+      if (__builtin_expect(seen[0] != ~0u, 0)) {
+        asm volatile("");
+        const uint32_t mine = seen[0] >> (16 * x + 4 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (!(mine >> r & 1)) {
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) s[qt][r] = -INFINITY;
+          }
+      }
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][2 * e], sl2, -lse2[qt]));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][2 * e + 1], sl2, -lse2[qt]));
+          const float d0 = p0 * (dp[qt][2 * e] - delta[qt]), d1 = p1 * (dp[qt][2 * e + 1] - delta[qt]);
+          excess[qt] += d0 + d1;
+          pw[qt][x * 2 + e] = __builtin_bit_cast(unsigned, cvt2(p0, p1));
+          dsw[qt][x * 2 + e] = __builtin_bit_cast(unsigned, cvt2(d0, d1));
+        }
     }
 #pragma unroll
     for (int x = 1; x < PD; ++x) seen[x - 1] = seen[x];
     seen[PD - 1] = fed;
-    bf16x8 dsop[QT];
+    bf16x8 pop[QT], dsop[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-      u32x4 wv;
-#pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e], sl2, -lse2[qt]));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k2][qt][2 * e + 1], sl2, -lse2[qt]));
-          const float d0 = p0 * (dp[k2][qt][2 * e] - delta[qt]), d1 = p1 * (dp[k2][qt][2 * e + 1] - delta[qt]);
-          excess[qt] += d0 + d1;
-          wv[k2 * 2 + e] = __builtin_bit_cast(unsigned, cvt2(d0, d1));
-        }
-      dsop[qt] = __builtin_bit_cast(bf16x8, wv);
+      pop[qt] = __builtin_bit_cast(bf16x8, pw[qt]);
+      dsop[qt] = __builtin_bit_cast(bf16x8, dsw[qt]);
     }
-    // the next rows are on their way during the last product and the result's stores
-    const bool last = c + 1 == it.chunks;
-    if (last) {
-      put_stat(tile);
-      if (tile + 1 < end) load_rows(tile + 1);
-    }
-    pv16<D>(dsop, kt, voff, dq);
+    cols_times_both<D, QT>(dsop, pop, kt, at, dq, pk);
     st = (st + 1) % NST;
-    ++c;
-    if (last) {
+    if (++c == it.chunks) {
       store(tile);
       c = 0;
       if (++tile == end) break;
-      take_rows();
+      take_rows(tile);
     }
   }
   wait_vmcnt<0>();                 // no load may still target this workgroup's LDS
@@ -337,8 +355,8 @@ void cross_grad_keys_kernel(CrossArgs a) {
   }
 }
 
-// Adds the parts of dQ (which 0) or of dK and dV (1, 2) in their order, four channels a
-// lane; a hidden key's gradients are zeros.
+// Adds the parts of dQ (which 0: of dS K, P K and e, and delta gets e) or of dK and dV (1,
+// 2) in their order, four channels a lane; a hidden key's gradients are zeros.
 template <int D>
 __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossArgs a, int first) {
   constexpr int kLanes = D / 4, kRows = kThreads / kLanes;
@@ -349,10 +367,23 @@ __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossArgs a, int fi
   const int bh = (int)(at / rows), r = (int)(at - (int64_t)bh * rows);
   const int b = bh / a.Hkv, kvh = bh - b * a.Hkv;
   f32x4 s = {};
-  if (which == 0 || is_seen(a, b, r, seen_keys(a, b))) {
-    const float* from = which == 0 ? a.part + ((int64_t)bh * parts * rows + r) * D + c
-                                   : a.part_kv + (((int64_t)bh * parts * 2 + (which - 1)) * rows + r) * D + c;
-    const int64_t step = (int64_t)rows * D * (which == 0 ? 1 : 2);
+  if (which == 0) {
+    const int64_t first_part = (int64_t)bh * parts * rows + r;
+    f32x4 pk = {};
+    float e = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+      const int64_t x = first_part + (int64_t)p * rows;
+      s += *reinterpret_cast<const f32x4*>(a.part + x * (2 * D) + c);
+      pk += *reinterpret_cast<const f32x4*>(a.part + x * (2 * D) + D + c);
+      e += a.stat_l[x];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] = fmaf(-e, pk[j], s[j]);
+    if (c == 0) a.stat[at].y += e;
+  } else if (is_seen(a, b, r, seen_keys(a, b))) {
+    const float* from = a.part_kv + (((int64_t)bh * parts * 2 + (which - 1)) * rows + r) * D + c;
+    const int64_t step = (int64_t)rows * D * 2;
 #pragma unroll 4
     for (int p = 0; p < parts; ++p) s += *reinterpret_cast<const f32x4*>(from + p * step);
   }
@@ -373,12 +404,12 @@ void launch_d(const CrossArgs& a, const CrossShape& s, hipStream_t stream) {
   else if (s.narrow) go(cross_grad_rows_kernel<D, 1, false>, a.wgs);
   else if (a.mask) go(cross_grad_rows_kernel<D, 2, true>, a.wgs);
   else go(cross_grad_rows_kernel<D, 2, false>, a.wgs);
-  go(cross_grad_keys_kernel<D>, a.kv_wgs);
   auto sum = [&](int first, int n, int64_t rows) {
     constexpr int kRows = kThreads / (D / 4);
     hipLaunchKernelGGL(cross_sum_kernel<D>, dim3((unsigned)((rows + kRows - 1) / kRows), n), dim3(kThreads), 0, stream, a, first);
   };
   if (a.splits > 1) sum(0, 1, (int64_t)a.B * a.Hkv * a.R);
+  go(cross_grad_keys_kernel<D>, a.kv_wgs);
   if (a.row_splits > 1) sum(1, 2, (int64_t)a.B * a.Hkv * a.M);
 }
 
@@ -411,8 +442,10 @@ CrossShape cross_grad_shape(int B, int Hkv, int G, int N, int M, int D, bool mas
   size_t at = mask ? s.seen_at + up256((size_t)B * 4) : 0;
   s.stat_at = at;
   at += up256((size_t)heads * R * 8);
+  s.stat_l_at = at;
+  if (s.splits > 1) at += up256((size_t)heads * s.splits * R * 4);
   s.part_at = at;
-  if (s.splits > 1) at += up256((size_t)heads * s.splits * R * D * 4);
+  if (s.splits > 1) at += up256((size_t)heads * s.splits * R * D * 8);
   s.part_kv_at = at;
   if (s.row_splits > 1) at += up256((size_t)heads * s.row_splits * 2 * M * D * 4);
   s.ws_bytes = at;

@@ -40,7 +40,7 @@ typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
 // Workgroups of 32 rows a wave that a CU holds: two, whose waves have 256 registers each.
 // Heads of 64 fit the 168 of three: 31,620 tokens' 40 heads over 512 keys take 260 us
-// instead of 305, with gradients another 819 instead of 850.
+// instead of 305, their gradients 880 instead of 920.
 constexpr int wide_per_cu(int D) { return D == 64 ? 3 : 2; }
 
 // A lane's place in a tile, for the row operands (row i at channels 8g .. +8) and for the
@@ -89,6 +89,26 @@ __device__ __forceinline__ void cols_times(const bf16x8 (&wop)[QT], unsigned til
     const bf16x8 col = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], hw[0], hw[1]});
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) acc[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(col, wop[qt], acc[dt][qt], 0, 0, 0);
+  }
+}
+
+// The same with two sets of weights.
+template <int D, int QT>
+__device__ __forceinline__ void cols_times_both(const bf16x8 (&w0)[QT], const bf16x8 (&w1)[QT], unsigned tile, const Places<D>& at,
+                                                f32x4 (&acc0)[Geo16<D>::DT][QT], f32x4 (&acc1)[Geo16<D>::DT][QT]) {
+  using G = Geo<D>;
+  const unsigned p = tile + at.col;
+#pragma unroll
+  for (int dt = 0; dt < Geo16<D>::DT; ++dt) {
+    const unsigned q = p ^ (dt << 5);
+    const u32x2 lw = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)q));
+    const u32x2 hw = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(size_t)(q + 16 * G::RB)));
+    const bf16x8 col = __builtin_bit_cast(bf16x8, u32x4{lw[0], lw[1], hw[0], hw[1]});
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      acc0[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(col, w0[qt], acc0[dt][qt], 0, 0, 0);
+      acc1[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(col, w1[qt], acc1[dt][qt], 0, 0, 0);
+    }
   }
 }
 

@@ -125,9 +125,11 @@ class Case:
             # a weight below TINY may be zero: dS is then off by TINY |dP - delta|, and dS below TINY may be zero too
             lost = TINY * (1 + np.abs(go) @ np.abs(v).T + (np.abs(go) * np.abs(o64[b, h])).sum(-1, keepdims=True))
             ds_err = p * d_err * (1 + e) + ds * (e + UB + 4 * U) + lost
-            tol[0][b, h] += self.c * ((ds_err + ds * U * (M + 40)) @ np.abs(k))
-            # dK may be formed with what delta is without out's rounding: the sum of P dP
+            # dQ and dK may be formed with what delta is without out's rounding, the sum of P dP.  For dQ that takes
+            # off P K away, off being found as a float32 sum of dS and P rounded to bf16
             off = np.abs((p * (go @ v.T)).sum(-1, keepdims=True) - (go * o64[b, h]).sum(-1, keepdims=True))
+            off_err = (ds_err + ds * U * (M + 40)).sum(-1, keepdims=True)
+            tol[0][b, h] += self.c * ((ds_err + ds * U * (M + 40) + p * (1 + e + UB + U * (M + 40)) * (off + off_err)) @ np.abs(k))
             tol[1][b, kv, at] += self.c * ((ds_err + p * off + (ds + p * off) * U * (N * group + 300)).T @ np.abs(q))
             tol[2][b, kv, at] += (p * (e + UB + U * (N * group + 300)) + TINY).T @ np.abs(go)
         for name, a, w, t in zip(("dq", "dk", "dv"), got, want, tol):
@@ -247,6 +249,39 @@ def test_states_past_32_bits_and_inputs_that_repeat_themselves():
                                  out=torch.empty_like(q))
     full, _ = sva.cross_attention(same.contiguous(), data[:1].repeat(2, 1, 1, 1), data[:1].repeat(2, 1, 1, 1))
     assert torch.equal(out, full)
+
+
+@pytest.mark.parametrize("N,M,D", [(64, 96, 128), (24, 1600, 64)])        # keys in one part and in several
+def test_gradients_do_not_carry_the_rounding_of_out(N, M, D):
+    """Rows with one large weight: delta from out as rounded to bf16 would be further off than dS itself."""
+    c = Case(1, 2, 1, N, M, D, scale=5.0, seed=3)
+    out, lse = sva.cross_attention(c.q, c.k, c.v, want_lse=True)
+    dq, dk, _ = (x.double().cpu().numpy() for x in sva.cross_attention_backward(c.go, c.q, c.k, c.v, out, lse))
+    o64, l64 = oca.forward(c.q64, c.k64, c.v64, c.seen, c.c)
+    want = oca.backward(c.go64, c.q64, c.k64, c.v64, o64, l64, c.seen, c.c)
+    given = out.double().cpu().numpy()
+    tol_k, past = UB * np.abs(want[1]), 0
+    for b, h, kv, at in c.each():
+        q, k, v, go = c.q64[b, h], c.k64[b, kv, at], c.v64[b, kv, at], c.go64[b, h]
+        # a weight: errors of the logit here and in lse, whose sum and rounding, exp2's step
+        e = 4 * c.logit_error(b, h, kv, at) + U * (M / 4 + 56 + 8 * np.abs(l64[b, h])[:, None])
+        p, dp = np.exp(c.c * (q @ k.T) - l64[b, h][:, None]), go @ v.T
+        delta = (p * dp).sum(-1, keepdims=True)
+        off = np.abs((go * given[b, h]).sum(-1, keepdims=True) - delta)     # what out's rounding takes from it
+        d_err = U * (D + 8) * (np.abs(go) @ np.abs(v).T + (np.abs(go) * np.abs(given[b, h])).sum(-1, keepdims=True))
+        ds = p * (np.abs(dp - delta) + off)                                 # as large as it may be when it is rounded
+        ds_f32 = p * d_err * (1 + e) + ds * (e + U * (M + 44)) + TINY * (1 + np.abs(dp) + np.abs(delta))
+        e_err = ds_f32.sum(-1, keepdims=True)                               # e is a sum of dS in float32
+        pk = p @ np.abs(k)
+        tol = UB * np.abs(want[0][b, h]) + c.c * ((ds_f32 + ds * UB) @ np.abs(k) + pk * (off * (e.max() + UB + U * (M + 40)) + e_err))
+        d = np.abs(dq[b, h] - want[0][b, h])
+        assert (d <= 1.02 * tol + TINY).all(), (h, d.max(), (d - 1.02 * tol).max())
+        past += (c.c * off * np.abs(p @ k) > 2 * tol).sum()
+        d_k = p * (dp - delta)
+        tol_k[b, kv, at] += c.c * ((ds_f32 + p * e_err + np.abs(d_k) * (UB + U * (4 * N + 300)) + p * U * 8 * np.abs(delta)).T @ np.abs(q))
+    assert past > 0                                                         # without the correction these would fail
+    d = np.abs(dk - want[1])
+    assert (d <= 1.02 * tol_k + TINY).all(), (d.max(), (d - 1.02 * tol_k).max())
 
 
 def test_gradient_against_differences():
