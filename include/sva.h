@@ -722,7 +722,8 @@ int sva_cross_attention(const sva_cross* p, const sva_heads* q, const sva_heads*
  *   dq, dk and dv lie apart from each other and from every input; hidden keys' rows of dk
  *   and dv are written with zeros, and rows of dq of an entry without keys
  * Weights and their gradients are rounded to bf16 for their products, sums are float32,
- * results are rounded once.  The same call gives the same bits. */
+ * results are rounded once; what out's rounding to bf16 takes from the rows' sums dO out is
+ * found and given back.  The same call gives the same bits. */
 int sva_cross_attention_backward(const sva_cross* p, const sva_heads* dout, const sva_heads* q, const sva_heads* k,
                                  const sva_heads* v, const sva_heads* out, const float* lse, const int32_t* lengths,
                                  const uint8_t* mask, int64_t mask_stride_b, void* workspace, size_t workspace_bytes,
