@@ -652,7 +652,8 @@ typedef struct sva_layer_norm_params {
 } sva_layer_norm_params;
 
 /* y = (x - mean) rstd w + bias, rstd = 1 / sqrt(var + eps), over a row's C channels (var
- * without Bessel's correction).
+ * without Bessel's correction).  More than 2^22 entries are SVA_ERR_SHAPE where they have
+ * weights of their own or their rows do not follow each other at one pitch.
  *   weight, bias : device, aligned to their elements, or NULL (ones, zeros)
  *   y            : may be x (same data and strides), must otherwise lie apart from it
  *   mean, rstd   : float32 [B, N] device, written, or NULL; what the gradient needs
@@ -679,7 +680,9 @@ int sva_layer_norm_backward(const sva_layer_norm_params* p, const sva_rows* dy, 
                             const float* mean, const float* rstd, void* workspace, size_t workspace_bytes,
                             const sva_rows* dx, float* dweight, float* dbias, void* stream);
 
-/* Cross attention: N query tokens, M states of an encoder. */
+/* Cross attention: N query tokens, M states of an encoder.  Sizes that a launch has no
+ * workgroups for (2^24 and more of B * Hkv, or of 128-key tiles of all of them; 2^22 and more
+ * entries with a mask) are SVA_ERR_SHAPE. */
 typedef struct sva_cross {
   int32_t batch;         /* B >= 1                                                  */
   int32_t heads;         /* H, a multiple of kv_heads; head h reads h / (H / Hkv)   */

@@ -310,8 +310,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_wave_kernel(NormArgs a) {
 // part; the waves' parts are joined as (count, mean, M2), one barrier a row.
 template <bool F32, bool ALIGNED, int V, int T>
 __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
-  constexpr int L = 0, PF = T > 512 ? 1 : 2;
-  const Place<L> at;
+  constexpr int PF = T > 512 ? 1 : 2;
+  const Place<0> at;
   const int C = a.C, b = blockIdx.x / a.parts, part = blockIdx.x - b * a.parts;
   __shared__ float2 joined[2][16];            // (mean, M2) of the waves' parts, two rows in turn
 
@@ -321,14 +321,9 @@ __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
   const Elem<F32>* xs = static_cast<const Elem<F32>*>(a.x.p) + b * a.x.sb;
   Elem<F32>* ys = static_cast<Elem<F32>*>(a.y.p) + b * a.y.sb;
 
-  // elements of this lane's part: the wave's own where a workgroup holds the row
   const int waves = blockDim.x / 64, wave = threadIdx.x / 64;
-  int mine = 0;                               // elements that this wave (L lanes) holds
-  if (L) {
-    mine = C;
-  } else {
-    for (int v = 0; v < V; ++v) mine += min(max(C - (v * at.step + wave * 64) * E, 0), 64 * E);
-  }
+  int mine = 0;                               // elements that this wave holds
+  for (int v = 0; v < V; ++v) mine += min(max(C - (v * at.step + wave * 64) * E, 0), 64 * E);
   const float inv_c = 1.0f / (float)C, inv_mine = mine ? 1.0f / (float)mine : 0.0f;
 
   // A row's loads go out PF rows ahead of its use: one row ahead left HBM waiting
@@ -338,7 +333,7 @@ __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
 #pragma unroll
   for (int u = 0; u < PF; ++u)
     if (n + (int64_t)u * stride < a.N) load_row<F32, ALIGNED, V>(xs + (n + (int64_t)u * stride) * a.x.sn, at.lane, at.step, C, ring[u]);
-  // (a workgroup's lanes are at the same row, or there is no barrier below)
+  // (a workgroup's lanes are at the same row)
   auto row = [&](Piece<F32> (&x)[V]) {
     float sum = 0.0f;
 #pragma unroll
@@ -348,7 +343,7 @@ __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) sum += f[e];
     }
-    float mean = lanes_sum<L ? L : 64>(sum) * inv_mine, m2 = 0.0f, dev = 0.0f;
+    float mean = lanes_sum<64>(sum) * inv_mine, m2 = 0.0f, dev = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float f[E];
@@ -361,30 +356,28 @@ __global__ __launch_bounds__(T) void norm_kernel(NormArgs a) {
       }
     }
     // what rounding left of the mean: the deviations' own
-    dev = lanes_sum<L ? L : 64>(dev);
-    m2 = lanes_sum<L ? L : 64>(m2);
+    dev = lanes_sum<64>(dev);
+    m2 = lanes_sum<64>(m2);
     const float more = dev * inv_mine;
     mean += more;
     m2 = fmaxf(m2 - dev * more, 0.0f);
-    if constexpr (L == 0) {
-      if (threadIdx.x % 64 == 0) joined[turn][wave] = make_float2(mean, m2);
-      __syncthreads();
-      // the mean of the waves' means around the first one's, then their squares around it
-      const float m0 = joined[turn][0].x;
-      float off = 0.0f;
-      for (int i = 0; i < waves; ++i) {
-        int count = 0;
-        for (int v = 0; v < V; ++v) count += min(max(C - (v * at.step + i * 64) * E, 0), 64 * E);
-        off = fmaf((float)count, joined[turn][i].x - m0, off);
-      }
-      mean = m0 + off * inv_c;
-      m2 = 0.0f;
-      for (int i = 0; i < waves; ++i) {
-        int count = 0;
-        for (int v = 0; v < V; ++v) count += min(max(C - (v * at.step + i * 64) * E, 0), 64 * E);
-        const float d = joined[turn][i].x - mean;
-        m2 += joined[turn][i].y + (float)count * d * d;
-      }
+    if (threadIdx.x % 64 == 0) joined[turn][wave] = make_float2(mean, m2);
+    __syncthreads();
+    // the mean of the waves' means around the first one's, then their squares around it
+    const float m0 = joined[turn][0].x;
+    float off = 0.0f;
+    for (int i = 0; i < waves; ++i) {
+      int count = 0;
+      for (int v = 0; v < V; ++v) count += min(max(C - (v * at.step + i * 64) * E, 0), 64 * E);
+      off = fmaf((float)count, joined[turn][i].x - m0, off);
+    }
+    mean = m0 + off * inv_c;
+    m2 = 0.0f;
+    for (int i = 0; i < waves; ++i) {
+      int count = 0;
+      for (int v = 0; v < V; ++v) count += min(max(C - (v * at.step + i * 64) * E, 0), 64 * E);
+      const float d = joined[turn][i].x - mean;
+      m2 += joined[turn][i].y + (float)count * d * d;
     }
     const float rstd = 1.0f / sqrtf(m2 * inv_c + a.eps);
     if (at.lane == 0) {

@@ -186,9 +186,10 @@ int sva_layer_norm_backward_workspace(const sva_layer_norm_params* p, size_t* by
   sva::NormShape s;
   size_t most = 0;
   for (int joined = 0; joined <= (p->per_entry ? 0 : 1); ++joined) {
-    if (norm_sizes(p, joined != 0, true, &a, &s) != SVA_OK) continue;
-    most = std::max(most, s.ws_bytes);
+    st = norm_sizes(p, joined != 0, true, &a, &s);       // (as one, any sizes will do)
+    if (st == SVA_OK) most = std::max(most, s.ws_bytes);
   }
+  if (st != SVA_OK) return st;
   *bytes = most;
   return SVA_OK;
 }

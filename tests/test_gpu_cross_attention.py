@@ -183,6 +183,13 @@ def test_rows_of_32_a_wave():
     Case(1, 66, 66, 1030, 20, 112, "mask").check()
 
 
+@pytest.mark.parametrize("hide", HIDE)
+def test_rows_of_32_a_wave_over_divided_keys(hide):
+    """Parts without a key where lengths are short, joined by a wave (few parts) or four."""
+    Case(3, 3, 1, 600, 3500, 112, hide).check()
+    Case(1, 1, 1, 1500, 2600, 64, hide, "token").check()
+
+
 @pytest.mark.parametrize("hide", ["none", "mask"])
 def test_large_logits_and_rising_ones(hide):
     """Logits of hundreds, the largest in the last key: the reference has to follow."""

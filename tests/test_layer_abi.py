@@ -144,6 +144,11 @@ def test_layer_norm_workspace(lib):
         assert need.value <= (4096 + p["batch"]) * p["channels"] * 8
     assert lib.sva_layer_norm_backward_workspace(LayerNormParams(**NORM), None) == BAD
     assert sva.layer_norm_backward_workspace(64, 1, 128, per_entry=True) == 0      # an entry's only row
+    # as many entries as a launch takes, one more, and as many rows that are one entry's
+    most = {**NORM, "batch": 1 << 22, "tokens": 1, "channels": 8}
+    assert lib.sva_layer_norm_backward_workspace(LayerNormParams(**{**most, "per_entry": 1}), need) == OK
+    assert lib.sva_layer_norm_backward_workspace(LayerNormParams(**{**most, "batch": (1 << 22) + 1, "per_entry": 1}), need) == SHAPE
+    assert lib.sva_layer_norm_backward_workspace(LayerNormParams(**{**most, "batch": (1 << 22) + 1, "per_entry": 0}), need) == OK
 
 
 # -------------------------------------------------------------- cross attention
