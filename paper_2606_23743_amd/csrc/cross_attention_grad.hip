@@ -161,6 +161,10 @@ void cross_grad_rows_kernel(CrossArgs a) {
       f32x4 s[QT], dp[QT];
       rows_times_half<D, QT>(s, kt + x * 16 * Geo<D>::RB, at, qop);
       rows_times_half<D, QT>(dp, vt + x * 16 * Geo<D>::RB, at, gop);
+      // Vector instructions may read a product eight wait states after its last instruction.
+      // Where the branch below comes between, the compiler has left them out (heads of 64, 16
+      // rows a wave), and S was read before it was there.
+      settle(s, dp);
       if (__builtin_expect(seen[0] != ~0u, 0)) {
         asm volatile("");
         const uint32_t mine = seen[0] >> (16 * x + 4 * g);

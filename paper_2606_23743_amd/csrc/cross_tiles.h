@@ -74,6 +74,13 @@ __device__ __forceinline__ void rows_times_half(f32x4 (&s)[QT], unsigned tile, c
   }
 }
 
+// eight wait states between products and whatever reads them
+template <int QT>
+__device__ __forceinline__ void settle(f32x4 (&x)[QT], f32x4 (&y)[QT]) {
+  if constexpr (QT == 1) asm volatile("s_nop 7" : "+v"(x[0]), "+v"(y[0]));
+  else asm volatile("s_nop 7" : "+v"(x[0]), "+v"(x[1]), "+v"(y[0]), "+v"(y[1]));
+}
+
 // acc += the tile's columns times the weights in registers, over its 32 rows in the order
 // of attn_w16.h
 template <int D, int QT>
