@@ -235,8 +235,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_wave_kernel(NormArgs a) {
     for (int e = 0; e < E; ++e) f[e] = e < left ? f[e] : 0.0f;
   };
   auto row = [&](Piece<F32> (&x)[V]) {
-    // Sums of float32 rows are of differences from the first element: a mean far from zero
-    // then costs the sum no digits (bf16 rows have none that it could cost).
+    // The sum of a float32 row is of differences from its first element: a mean far from zero
+    // then costs it no digits (bf16 rows have none that it could cost).  Where the first is far
+    // from the others the differences have lost theirs, so deviations are of the row itself,
+    // and what their sum leaves is the mean's error, which they and the mean are rid of: rows of
+    // 4,096 whose first channel is 1e5 had lost up to 0.4 % of a deviation in every other.
     float f[V][E], sum = 0.0f, first = 0.0f;
     if constexpr (F32) first = __shfl(__uint_as_float(x[0].w[0]), 0, L);
 #pragma unroll
@@ -245,15 +248,31 @@ __global__ __launch_bounds__(kNormThreads) void norm_wave_kernel(NormArgs a) {
       widen<F32>(x[v], f[v]);
       if (c < C) {
         if constexpr (F32) {
+          float d[E];
 #pragma unroll
-          for (int e = 0; e < E; ++e) f[v][e] -= first;
-          clear_tail(f[v], v);
+          for (int e = 0; e < E; ++e) d[e] = f[v][e] - first;
+          clear_tail(d, v);
+          sum += sum8(d);
+        } else {
+          sum += sum8(f[v]);
         }
-        sum += sum8(f[v]);
       }
     }
-    const float off = lanes_sum<L>(sum) * inv_c, mean = first + off;
-    float m2 = 0.0f;
+    float mean = first + lanes_sum<L>(sum) * inv_c, more = 0.0f, m2 = 0.0f;
+    if constexpr (F32) {
+      float dev = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if ((lane + v * L) * E < C) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[v][e] -= mean;
+          clear_tail(f[v], v);
+          dev += sum8(f[v]);
+        }
+      more = lanes_sum<L>(dev) * inv_c;
+    }
+    const float off = F32 ? more : mean;
+    mean += more;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (lane + v * L) * E;
