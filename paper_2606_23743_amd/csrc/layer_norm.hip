@@ -481,10 +481,19 @@ __global__ __launch_bounds__(T) void norm_grad_kernel(NormArgs a) {
       for (int v = 0; v < V; ++v) {
         widen<F32>(r[k].x[v], f[k][v]);
         widen<F32>(r[k].g[v], d[k][v]);
+        // Past the row's end x and dy are zero; so is xhat there, as a mean times rstd may be
+        // infinite where no element of the row is far from it.
+        int left = C - (at.lane + v * at.step) * E;
+        const float mean = ALIGNED && left <= 0 ? 0.0f : r[k].mean;
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[k][v][e] = (f[k][v][e] - mean) * r[k].rstd;       // xhat
+        if (!ALIGNED && (v + 1) * at.step * E > C) {
+          asm volatile("" : "+v"(left));       // (not eight masks kept from row to row)
+#pragma unroll
+          for (int e = 0; e < E; ++e) f[k][v][e] = e < left ? f[k][v][e] : 0.0f;
+        }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          // past the row's end dy is zero, and so are all four
-          f[k][v][e] = (f[k][v][e] - r[k].mean) * r[k].rstd;       // xhat
           dw[v][e] = fmaf(d[k][v][e], f[k][v][e], dw[v][e]);
           db[v][e] += d[k][v][e];
           d[k][v][e] *= w[v][e];                                   // g
