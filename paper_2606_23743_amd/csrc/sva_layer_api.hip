@@ -29,7 +29,7 @@ int check_rows3(const sva_rows* r, int64_t B, int64_t N, int64_t C, size_t item,
 int check_norm(const sva_layer_norm_params* p) {
   if (!p || p->batch < 1 || p->tokens < 1 || p->channels < 1) return SVA_ERR_INVALID_ARG;
   if (!good_dtype(p->dtype) || !good_dtype(p->weight_dtype)) return SVA_ERR_INVALID_ARG;
-  if (!isfinite(p->eps) || !((float)p->eps >= FLT_MIN)) return SVA_ERR_INVALID_ARG;
+  if (!((float)p->eps >= FLT_MIN && (float)p->eps <= FLT_MAX)) return SVA_ERR_INVALID_ARG;
   if (p->weight_stride_b < 0 || p->bias_stride_b < 0) return SVA_ERR_INVALID_ARG;
   if (p->channels > sva::kNormMaxChannels) return SVA_ERR_UNSUPPORTED;
   if ((int64_t)p->batch * p->tokens > INT32_MAX - (1 << 20)) return SVA_ERR_SHAPE;

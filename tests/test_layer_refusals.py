@@ -1,0 +1,31 @@
+"""Calls of layer norm and cross attention that are refused before any HIP call: values past
+float32, launches past 2^32 threads, outputs that share memory with what is read or written
+beside them.  Addresses are never dereferenced."""
+import pytest
+
+from paper_2606_23743_amd import _lib
+from paper_2606_23743_amd._lib import LayerNormParams, Rows
+
+pytestmark = pytest.mark.cpu
+
+A, MB = 1 << 30, 1 << 24
+OK, BAD, SHAPE = _lib.SVA_OK, _lib.SVA_ERR_INVALID_ARG, _lib.SVA_ERR_SHAPE
+NORM = dict(batch=2, tokens=5, channels=64, dtype=0, weight_dtype=1, per_entry=0, unit_offset=0, weight_stride_b=0,
+            bias_stride_b=0, eps=1e-5)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return _lib.load()
+
+
+def rows(at, n=5, c=64):
+    return Rows(at, n * c, c)
+
+
+@pytest.mark.parametrize("eps", [3.5e38, 1e300])
+def test_an_eps_past_float32(lib, eps):
+    """As float32 it would be infinite, and every row its bias."""
+    p = LayerNormParams(**{**NORM, "eps": eps})
+    assert lib.sva_layer_norm(p, rows(A), None, None, rows(A + MB + 1), None, None, None) == BAD     # (before y's alignment)
+    assert lib.sva_layer_norm_backward_workspace(p, _lib.ctypes.c_size_t()) == BAD
