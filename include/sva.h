@@ -652,8 +652,9 @@ typedef struct sva_layer_norm_params {
 } sva_layer_norm_params;
 
 /* y = (x - mean) rstd w + bias, rstd = 1 / sqrt(var + eps), over a row's C channels (var
- * without Bessel's correction).  More than 2^22 entries are SVA_ERR_SHAPE where they have
- * weights of their own or their rows do not follow each other at one pitch.
+ * without Bessel's correction).  More than 2^22 entries (of more than 15,360 channels: 2^22
+ * and more) are SVA_ERR_SHAPE where they have weights of their own or their rows do not
+ * follow each other at one pitch.
  *   weight, bias : device, aligned to their elements, or NULL (ones, zeros)
  *   y            : may be x (same data and strides), must otherwise lie apart from it
  *   mean, rstd   : float32 [B, N] device, written, or NULL; what the gradient needs

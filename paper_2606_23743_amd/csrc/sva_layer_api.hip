@@ -50,7 +50,9 @@ int norm_sizes(const sva_layer_norm_params* p, bool joined, bool grad, sva::Norm
   a->N = joined ? p->batch * p->tokens : p->tokens;
   a->C = p->channels;
   *s = sva::norm_shape(a->B, a->N, a->C, grad, joined || p->per_entry != 0);
-  if ((int64_t)a->B * s->parts > 1 << 22) return SVA_ERR_SHAPE;   // a launch's workgroups
+  // a launch has 2^22 workgroups at most, and fewer than 2^32 threads
+  const int64_t wgs = (int64_t)a->B * s->parts;
+  if (wgs > 1 << 22 || wgs * s->threads >= (int64_t)1 << 32) return SVA_ERR_SHAPE;
   a->parts = s->parts;
   return SVA_OK;
 }

@@ -29,3 +29,20 @@ def test_an_eps_past_float32(lib, eps):
     p = LayerNormParams(**{**NORM, "eps": eps})
     assert lib.sva_layer_norm(p, rows(A), None, None, rows(A + MB + 1), None, None, None) == BAD     # (before y's alignment)
     assert lib.sva_layer_norm_backward_workspace(p, _lib.ctypes.c_size_t()) == BAD
+
+
+@pytest.mark.parametrize("per_entry", [0, 1])
+def test_launches_past_32_bits_of_threads(lib, per_entry):
+    """2^22 entries of their own in workgroups of 1,024 threads; one entry fewer, or fewer threads, are a launch."""
+    B, need = 1 << 22, _lib.ctypes.c_size_t()
+
+    def asked(batch, channels):
+        return lib.sva_layer_norm_backward_workspace(LayerNormParams(**{**NORM, "batch": batch, "tokens": 1, "channels": channels,
+                                                                        "per_entry": 1}), need)
+
+    assert asked(B, 16384) == SHAPE and asked(B, 15361) == SHAPE
+    assert asked(B - 1, 16384) == OK and asked(B, 15360) == OK and asked(B, 8) == OK
+    p = LayerNormParams(**{**NORM, "batch": B, "tokens": 2, "channels": 16384, "per_entry": per_entry})
+    x, y = Rows(A, 0, 0), Rows(A + MB, 3 * 16384, 16384)                       # (no pitch of all rows)
+    assert lib.sva_layer_norm(p, x, None, None, y, None, None, None) == SHAPE
+    assert lib.sva_layer_norm_backward(p, x, x, None, A, A, A, 1 << 60, y, A, A + MB, None) == SHAPE
