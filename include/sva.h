@@ -702,7 +702,8 @@ int sva_cross_attention_workspace(const sva_cross* p, int32_t masked, size_t* by
 int sva_cross_attention_backward_workspace(const sva_cross* p, int32_t masked, size_t* bytes);
 
 /* out = softmax(c Q K^T) V over the keys that an entry has.
- *   q, out  : bf16 [B, H, N, D]; out apart from every input
+ *   q, out  : bf16 [B, H, N, D]; out and lse share no byte with each other or an input (rows
+ *             of tensors may interleave, as slices of one projection do)
  *   k, v    : bf16 [B, Hkv, M, D]
  *   lengths : int32 [B] device or NULL (M): keys 0 .. lengths[b]-1, clamped to [0, M]
  *   mask    : uint8 device or NULL: key m of entry b is seen where mask[b * mask_stride_b
@@ -710,7 +711,8 @@ int sva_cross_attention_backward_workspace(const sva_cross* p, int32_t masked, s
  *   lse     : float32 [B, H, N] contiguous or NULL: natural-log log-sum-exp of the scaled
  *             logits
  *   workspace : 256-byte aligned, may be NULL where none is needed; contents on entry do
- *             not matter.  Calls that share one must not overlap.
+ *             not matter.  Calls that share one must not overlap; it shares no byte with
+ *             what else the call takes.
  * Tensors by strides, 16-byte aligned data and strides.  Hidden keys and values take no
  * part, whatever they hold; a query of an entry without keys gets zeros and an lse of
  * -inf.  Products are bf16 MFMA with float32 accumulation; weights are rounded to bf16
@@ -723,8 +725,9 @@ int sva_cross_attention(const sva_cross* p, const sva_heads* q, const sva_heads*
 /* Gradients of q, k and v from dout, the gradient of out, with out and lse as
  * sva_cross_attention wrote them for the same arguments.
  *   dout, dq : bf16 [B, H, N, D]; dk, dv: bf16 [B, Hkv, M, D], summed over a group's heads
- *   dq, dk and dv lie apart from each other and from every input; hidden keys' rows of dk
- *   and dv are written with zeros, and rows of dq of an entry without keys
+ *   dq, dk and dv share no byte with each other or an input (their rows may interleave);
+ *   hidden keys' rows of dk and dv are written with zeros, and rows of dq of an entry without
+ *   keys
  * Weights and their gradients are rounded to bf16 for their products, sums are float32,
  * results are rounded once; what out's rounding to bf16 takes from the rows' sums dO out is
  * found and given back.  The same call gives the same bits. */

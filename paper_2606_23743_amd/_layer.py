@@ -286,8 +286,9 @@ def cross_attention(q, k, v, lengths=None, mask=None, softmax_scale: float = 0.0
     [B, kv_heads, M, D] (N and M from one on; H a multiple of kv_heads),
     sva_cross_attention.  lengths: int32 [B], an entry's keys; mask: uint8 or bool [B, M]
     or [M], nonzero where a key is seen.  q, k, v and out take any strides with contiguous
-    channels that are multiples of 16 bytes; out is made like q.  want_lse: float32
-    [B, H, N], which cross_attention_backward takes.  workspace: a uint8 device tensor of
+    channels that are multiples of 16 bytes; out is made like q, and shares no byte with what
+    is read (slices of one projection may interleave).  want_lse: float32 [B, H, N], which
+    cross_attention_backward takes.  workspace: a uint8 device tensor of
     cross_attention_workspace bytes (allocated when None).  Returns (out, lse)."""
     torch = _torch()
     dev, prm, rows, states, lens, mk, mask_b = _cross(q, k, lengths, mask, softmax_scale)
@@ -310,8 +311,8 @@ def cross_attention(q, k, v, lengths=None, mask=None, softmax_scale: float = 0.0
 def cross_attention_backward(dout, q, k, v, out, lse, lengths=None, mask=None, softmax_scale: float = 0.0, dq=None, dk=None,
                              dv=None, workspace=None, stream=None) -> Tuple:
     """Gradients of q, k and v, like them, from dout (like out), with out and lse as
-    cross_attention gave them for the same arguments, sva_cross_attention_backward.
-    workspace: a uint8 device tensor of cross_attention_workspace(..., backward=True)
+    cross_attention gave them for the same arguments, sva_cross_attention_backward.  dq, dk
+    and dv share no byte with each other or with what is read.  workspace: a uint8 device tensor of cross_attention_workspace(..., backward=True)
     bytes (allocated when None).  Returns (dq, dk, dv)."""
     torch = _torch()
     dev, prm, rows, states, lens, mk, mask_b = _cross(q, k, lengths, mask, softmax_scale)

@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "../../include/sva.h"
+#include "overlap.h"
 #include "sva_internal.h"
 
 namespace sva {
@@ -23,6 +24,7 @@ struct Tensor {
   HeadsView v;
   size_t span;
   int align;                     // what data and strides are multiples of: 16, 8, 4 or 2 bytes
+  RowSet rows;
 };
 
 inline int check_heads(const sva_heads* h, int64_t B, int64_t N, int64_t D, size_t item, bool wide, bool output, Tensor* t) {
@@ -63,6 +65,12 @@ inline int check_heads(const sva_heads* h, int64_t B, int64_t N, int64_t D, size
   t->v.heads = h->heads;
   t->span = (size_t)span * item;
   t->align = align;
+  t->rows.at = reinterpret_cast<uintptr_t>(h->data);
+  t->rows.row = D * (int64_t)item;
+  for (int i = 0; i < 3; ++i) {
+    t->rows.size[i] = dims[i].size;
+    t->rows.stride[i] = dims[i].stride * (int64_t)item;
+  }
   return SVA_OK;
 }
 
@@ -70,6 +78,18 @@ inline bool apart(const Tensor& x, const Tensor& y) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(x.v.p), b = reinterpret_cast<uintptr_t>(y.v.p);
   return a + x.span <= b || b + y.span <= a;
 }
+
+// `rows` runs of `row` bytes as a tensor.
+inline Tensor runs_of(const void* p, int64_t rows, int64_t stride, int64_t row) {
+  Tensor t{};
+  t.v.p = const_cast<void*>(p);
+  t.span = (size_t)((rows - 1) * stride + row);
+  t.rows = {reinterpret_cast<uintptr_t>(p), row, {rows, 1, 1}, {stride, 0, 0}};
+  return t;
+}
+
+// Whether they share a byte: apart() by rows, not by spans.
+inline bool meet(const Tensor& x, const Tensor& y) { return !apart(x, y) && rows_meet(x.rows, y.rows); }
 
 inline bool same(const Tensor& x, const Tensor& y, int64_t B, int64_t N) {
   return x.v.p == y.v.p && (B == 1 || x.v.sb == y.v.sb) && (x.v.heads == 1 || x.v.sh == y.v.sh) &&

@@ -140,6 +140,23 @@ int check_workspace(void* workspace, size_t bytes, size_t need) {
   return aligned(workspace, 256) ? SVA_OK : SVA_ERR_ALIGNMENT;
 }
 
+// What a call writes has to lie apart from all that it reads and writes beside it, as it is
+// written while other workgroups still read: the first `written` of `count`.
+bool shares(const Tensor* const* all, int written, int count) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < count; ++j)
+      if (all[i]->v.p && all[j]->v.p && meet(*all[i], *all[j])) return true;
+  return false;
+}
+
+Tensor lengths_of(const sva_cross* p, const int32_t* lengths) { return runs_of(lengths, 1, 0, (int64_t)p->batch * 4); }
+Tensor mask_of(const sva_cross* p, const uint8_t* mask, int64_t stride_b) {
+  return runs_of(mask, p->batch, p->batch > 1 ? stride_b : 0, p->keys);
+}
+Tensor lse_of(const sva_cross* p, const float* lse) {
+  return runs_of(lse, 1, 0, (int64_t)p->batch * p->heads * p->queries * 4);
+}
+
 void place_workspace(void* workspace, const sva::CrossShape& s, sva::CrossArgs* a) {
   unsigned char* w = static_cast<unsigned char*>(workspace);
   a->bits = reinterpret_cast<uint32_t*>(w + s.bits_at);
@@ -257,10 +274,12 @@ int sva_cross_attention(const sva_cross* p, const sva_heads* q, const sva_heads*
   if ((st = check_cross_tensor(p, k, true, false, &tk)) != SVA_OK) return st;
   if ((st = check_cross_tensor(p, v, true, false, &tv)) != SVA_OK) return st;
   if ((st = check_cross_tensor(p, out, false, true, &to)) != SVA_OK) return st;
-  // outputs are written while other workgroups still read the inputs
-  if (to.v.p == tq.v.p || to.v.p == tk.v.p || to.v.p == tv.v.p) return SVA_ERR_INVALID_ARG;
   if (!aligned(lse, 4)) return SVA_ERR_ALIGNMENT;
   if ((st = check_workspace(workspace, workspace_bytes, s.ws_bytes)) != SVA_OK) return st;
+  const Tensor tl = lse_of(p, lse), tn = lengths_of(p, lengths), tm = mask_of(p, mask, mask_stride_b);
+  const Tensor tw = runs_of(s.ws_bytes ? workspace : nullptr, 1, 0, (int64_t)s.ws_bytes);
+  const Tensor* all[] = {&to, &tl, &tw, &tq, &tk, &tv, &tn, &tm};
+  if (shares(all, 3, 8)) return SVA_ERR_INVALID_ARG;
   a.q = tq.v;
   a.k = tk.v;
   a.v = tv.v;
@@ -301,14 +320,12 @@ int sva_cross_attention_backward(const sva_cross* p, const sva_heads* dout, cons
   if ((st = check_cross_tensor(p, dq, false, true, &dtq)) != SVA_OK) return st;
   if ((st = check_cross_tensor(p, dk, true, true, &dtk)) != SVA_OK) return st;
   if ((st = check_cross_tensor(p, dv, true, true, &dtv)) != SVA_OK) return st;
-  const void* outputs[3] = {dtq.v.p, dtk.v.p, dtv.v.p};
-  for (int i = 0; i < 3; ++i) {
-    for (const Tensor* t : {&tg, &tq, &tk, &tv, &to})
-      if (outputs[i] == t->v.p) return SVA_ERR_INVALID_ARG;
-    if (outputs[i] == outputs[(i + 1) % 3]) return SVA_ERR_INVALID_ARG;
-  }
   if (!aligned(lse, 4)) return SVA_ERR_ALIGNMENT;
   if ((st = check_workspace(workspace, workspace_bytes, s.ws_bytes)) != SVA_OK) return st;
+  const Tensor tl = lse_of(p, lse), tn = lengths_of(p, lengths), tm = mask_of(p, mask, mask_stride_b);
+  const Tensor tw = runs_of(s.ws_bytes ? workspace : nullptr, 1, 0, (int64_t)s.ws_bytes);
+  const Tensor* all[] = {&dtq, &dtk, &dtv, &tw, &tg, &tq, &tk, &tv, &to, &tl, &tn, &tm};
+  if (shares(all, 4, 12)) return SVA_ERR_INVALID_ARG;
   a.dout = tg.v;
   a.q = tq.v;
   a.k = tk.v;

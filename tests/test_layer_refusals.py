@@ -4,7 +4,7 @@ beside them.  Addresses are never dereferenced."""
 import pytest
 
 from paper_2606_23743_amd import _lib
-from paper_2606_23743_amd._lib import LayerNormParams, Rows
+from paper_2606_23743_amd._lib import Cross, Heads, LayerNormParams, Rows
 
 pytestmark = pytest.mark.cpu
 
@@ -46,3 +46,71 @@ def test_launches_past_32_bits_of_threads(lib, per_entry):
     x, y = Rows(A, 0, 0), Rows(A + MB, 3 * 16384, 16384)                       # (no pitch of all rows)
     assert lib.sva_layer_norm(p, x, None, None, y, None, None, None) == SHAPE
     assert lib.sva_layer_norm_backward(p, x, x, None, A, A, A, 1 << 60, y, A, A + MB, None) == SHAPE
+
+
+# ---- cross attention: outputs that share memory ----
+
+B, H, KV, N, M, D = 2, 4, 2, 5, 9, 64
+
+
+def _cross(**kw):
+    """Arguments of both calls, all apart (and the mask and workspace large)."""
+    at = iter(A + i * MB for i in range(20))
+    q = lambda: _rows(next(at))  # noqa: E731
+    k = lambda: Heads(next(at), KV, KV * M * D, M * D, D)  # noqa: E731
+    t = dict(q=q(), k=k(), v=k(), out=q(), dout=q(), dq=q(), dk=k(), dv=k(), lse=next(at), lens=next(at), mask=next(at), ws=next(at))
+    return {**t, **{n: f(t) for n, f in kw.items()}}
+
+
+def _rows(at):
+    return Heads(at, H, H * N * D, N * D, D)
+
+
+def _moved(x, elements):
+    return Heads(x.data + 2 * elements, x.heads, x.stride_b, x.stride_h, x.stride_n)
+
+
+FORWARD = {
+    "out is q one token on": dict(out=lambda t: _moved(t["q"], D)),
+    "out is q one token back": dict(out=lambda t: _moved(t["q"], -D)),
+    "out is q one head on": dict(out=lambda t: _moved(t["q"], N * D)),
+    "out ends in k": dict(out=lambda t: _rows(t["k"].data - 2 * (B * H * N - 1) * D)),
+    "out begins at v's last row": dict(out=lambda t: _rows(t["v"].data + 2 * (B * KV * M - 1) * D)),
+    "lse in q": dict(lse=lambda t: t["q"].data + 64),
+    "lse in out": dict(lse=lambda t: t["out"].data + 64),
+    "lse over the lengths": dict(lse=lambda t: t["lens"] - 8),
+    "out over the mask": dict(out=lambda t: _rows(t["mask"] + 16 - 2 * B * H * N * D)),
+    "workspace in v": dict(ws=lambda t: t["v"].data + 256),
+    "workspace over out": dict(ws=lambda t: t["out"].data),
+}
+BACKWARD = {
+    "dq is q one token on": dict(dq=lambda t: _moved(t["q"], D)),
+    "dq is dout one token on": dict(dq=lambda t: _moved(t["dout"], D)),
+    "dq is out one token back": dict(dq=lambda t: _moved(t["out"], -D)),
+    "dk is k one row on": dict(dk=lambda t: _moved(t["k"], D)),
+    "dv is v one head on": dict(dv=lambda t: _moved(t["v"], M * D)),
+    "dk is dv one row on": dict(dk=lambda t: _moved(t["dv"], D)),
+    "dv begins in dq": dict(dv=lambda t: Heads(t["dq"].data + 16, KV, KV * M * D, M * D, D)),
+    "dq over the lse": dict(dq=lambda t: _rows(t["lse"])),
+    "workspace over dk": dict(ws=lambda t: t["dk"].data),
+}
+
+
+def _forward(lib, t):
+    return lib.sva_cross_attention(Cross(B, H, KV, N, M, D, 0.0), t["q"], t["k"], t["v"], t["lens"], t["mask"], M, t["ws"],
+                                   1 << 20, t["out"], t["lse"], None)
+
+
+def _backward(lib, t):
+    return lib.sva_cross_attention_backward(Cross(B, H, KV, N, M, D, 0.0), t["dout"], t["q"], t["k"], t["v"], t["out"], t["lse"],
+                                            t["lens"], t["mask"], M, t["ws"], 1 << 20, t["dq"], t["dk"], t["dv"], None)
+
+
+@pytest.mark.parametrize("name", FORWARD)
+def test_cross_attention_outputs_apart(lib, name):
+    assert _forward(lib, _cross(**FORWARD[name])) == BAD
+
+
+@pytest.mark.parametrize("name", BACKWARD)
+def test_cross_attention_gradients_apart(lib, name):
+    assert _backward(lib, _cross(**BACKWARD[name])) == BAD
