@@ -658,6 +658,7 @@ typedef struct sva_layer_norm_params {
  *   weight, bias : device, aligned to their elements, or NULL (ones, zeros)
  *   y            : may be x (same data and strides), must otherwise lie apart from it
  *   mean, rstd   : float32 [B, N] device, written, or NULL; what the gradient needs
+ * What is written shares no byte with anything else that the call takes.
  * Data aligned to their elements; accesses are of whole 16 bytes where data and strides
  * are multiples of 16 bytes and C of 8.  Sums are float32, squares are of deviations from
  * the mean; y is rounded once. */
@@ -676,6 +677,7 @@ int sva_layer_norm_backward_workspace(const sva_layer_norm_params* p, size_t* by
  *   mean, rstd : float32 [B, N], as sva_layer_norm wrote them
  *   workspace  : 256-byte aligned, at least sva_layer_norm_backward_workspace bytes; not
  *                read where neither sum is wanted.  Calls that share one must not overlap.
+ * dx, the sums and the workspace share no byte with anything else that the call takes.
  * Sums are float32 in a fixed order: the same call gives the same bits. */
 int sva_layer_norm_backward(const sva_layer_norm_params* p, const sva_rows* dy, const sva_rows* x, const void* weight,
                             const float* mean, const float* rstd, void* workspace, size_t workspace_bytes,

@@ -17,6 +17,15 @@ namespace {
 
 using namespace sva::api;
 
+// What a call writes has to lie apart from all that it reads and writes beside it, as it is
+// written while other workgroups still read: the first `written` of `count`.
+bool shares(const Tensor* const* all, int written, int count) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < count; ++j)
+      if (all[i]->v.p && all[j]->v.p && meet(*all[i], *all[j])) return true;
+  return false;
+}
+
 // ---- layer norm ----
 
 // One tensor [B, N, C] as a tensor of one head.
@@ -66,6 +75,16 @@ void norm_weights(const sva_layer_norm_params* p, const void* weight, const void
   a->unit = p->unit_offset ? 1.0f : 0.0f;
   a->eps = (float)p->eps;
   a->f32 = p->dtype == SVA_F32;
+}
+
+Tensor weight_of(const sva_layer_norm_params* p, const void* w, int64_t stride_b) {
+  const int64_t item = (int64_t)item_of(p->weight_dtype);
+  const bool rows = p->per_entry && p->batch > 1;
+  return runs_of(w, rows ? p->batch : 1, rows ? stride_b * item : 0, p->channels * item);
+}
+Tensor stat_of(const sva_layer_norm_params* p, const float* s) { return runs_of(s, 1, 0, (int64_t)p->batch * p->tokens * 4); }
+Tensor sum_of(const sva_layer_norm_params* p, const float* s) {
+  return runs_of(s, 1, 0, (int64_t)(p->per_entry ? p->batch : 1) * p->channels * 4);
 }
 
 // ---- cross attention ----
@@ -140,15 +159,6 @@ int check_workspace(void* workspace, size_t bytes, size_t need) {
   return aligned(workspace, 256) ? SVA_OK : SVA_ERR_ALIGNMENT;
 }
 
-// What a call writes has to lie apart from all that it reads and writes beside it, as it is
-// written while other workgroups still read: the first `written` of `count`.
-bool shares(const Tensor* const* all, int written, int count) {
-  for (int i = 0; i < written; ++i)
-    for (int j = i + 1; j < count; ++j)
-      if (all[i]->v.p && all[j]->v.p && meet(*all[i], *all[j])) return true;
-  return false;
-}
-
 Tensor lengths_of(const sva_cross* p, const int32_t* lengths) { return runs_of(lengths, 1, 0, (int64_t)p->batch * 4); }
 Tensor mask_of(const sva_cross* p, const uint8_t* mask, int64_t stride_b) {
   return runs_of(mask, p->batch, p->batch > 1 ? stride_b : 0, p->keys);
@@ -187,6 +197,10 @@ int sva_layer_norm(const sva_layer_norm_params* p, const sva_rows* x, const void
   sva::NormArgs a{};
   sva::NormShape s;
   if ((st = norm_sizes(p, joined, false, &a, &s)) != SVA_OK) return st;
+  const Tensor tw = weight_of(p, weight, p->weight_stride_b), tb = weight_of(p, bias, p->bias_stride_b);
+  const Tensor tm = stat_of(p, mean), tr = stat_of(p, rstd);
+  const Tensor *stats[] = {&tm, &tr, &ty, &tx, &tw, &tb}, *result[] = {&ty, &tw, &tb};
+  if (shares(stats, 2, 6) || shares(result, 1, 3)) return SVA_ERR_INVALID_ARG;
   norm_weights(p, weight, bias, &a);
   a.x = view(tx, joined, N);
   a.y = view(ty, joined, N);
@@ -229,13 +243,17 @@ int sva_layer_norm_backward(const sva_layer_norm_params* p, const sva_rows* dy, 
   if ((weight && !aligned(weight, item_of(p->weight_dtype))) || !aligned(mean, 4) || !aligned(rstd, 4) ||
       !aligned(dweight, 4) || !aligned(dbias, 4))
     return SVA_ERR_ALIGNMENT;
-  if (dweight && dweight == dbias) return SVA_ERR_INVALID_ARG;
   const bool joined = !p->per_entry && one_run(tx, B, N) && one_run(tg, B, N) && one_run(to, B, N);
   sva::NormArgs a{};
   sva::NormShape s;
   if ((st = norm_sizes(p, joined, true, &a, &s)) != SVA_OK) return st;
   const bool sums = dweight || dbias;
   if (sums && (st = check_workspace(workspace, workspace_bytes, s.ws_bytes)) != SVA_OK) return st;
+  const Tensor tw = weight_of(p, weight, p->weight_stride_b), tm = stat_of(p, mean), tr = stat_of(p, rstd);
+  const Tensor tdw = sum_of(p, dweight), tdb = sum_of(p, dbias);
+  const Tensor ts = runs_of(sums && s.ws_bytes ? workspace : nullptr, 1, 0, (int64_t)s.ws_bytes);
+  const Tensor *all[] = {&tdw, &tdb, &ts, &to, &tg, &tx, &tw, &tm, &tr}, *result[] = {&to, &tw, &tm, &tr};
+  if (shares(all, 3, 9) || shares(result, 1, 4)) return SVA_ERR_INVALID_ARG;
   norm_weights(p, weight, nullptr, &a);
   a.x = view(tx, joined, N);
   a.dy = view(tg, joined, N);

@@ -114,3 +114,51 @@ def test_cross_attention_outputs_apart(lib, name):
 @pytest.mark.parametrize("name", BACKWARD)
 def test_cross_attention_gradients_apart(lib, name):
     assert _backward(lib, _cross(**BACKWARD[name])) == BAD
+
+
+# ---- layer norm: the same ----
+
+TOKENS = 900                                             # (workgroups to be joined: a workspace)
+
+
+def _norm(**kw):
+    at = iter(A + i * MB for i in range(20))
+    t = dict(**{n: rows(next(at), TOKENS) for n in ("x", "y", "dy", "dx")}, **{n: next(at) for n in (
+        "w", "b", "mean", "rstd", "dw", "db", "ws")})
+    return {**t, **{n: f(t) for n, f in kw.items()}}
+
+
+NORM_FORWARD = {
+    "mean is rstd": dict(mean=lambda t: t["rstd"]),
+    "mean ends in rstd": dict(mean=lambda t: t["rstd"] - 4),
+    "rstd in y": dict(rstd=lambda t: t["y"].data + 4),
+    "mean in x": dict(mean=lambda t: t["x"].data + 4),
+    "rstd in the weight": dict(rstd=lambda t: t["w"] + 4),
+    "y over the bias": dict(y=lambda t: rows(t["b"], TOKENS)),
+    "y ends in the weight": dict(y=lambda t: rows(t["w"] - 2 * 2 * TOKENS * 64 + 2, TOKENS)),
+}
+NORM_BACKWARD = {
+    "the sums are one": dict(dw=lambda t: t["db"]),
+    "the sums overlap": dict(dw=lambda t: t["db"] + 4),
+    "a sum in dy": dict(dw=lambda t: t["dy"].data),
+    "a sum in dx": dict(db=lambda t: t["dx"].data + 4),
+    "a sum over the weight": dict(dw=lambda t: t["w"]),
+    "dx over the mean": dict(dx=lambda t: rows(t["mean"], TOKENS)),
+    "dx over the weight": dict(dx=lambda t: rows(t["w"], TOKENS)),
+    "workspace over a sum": dict(ws=lambda t: t["dw"]),
+    "workspace over x": dict(ws=lambda t: t["x"].data),
+}
+
+
+@pytest.mark.parametrize("name", NORM_FORWARD)
+def test_layer_norm_outputs_apart(lib, name):
+    t = _norm(**NORM_FORWARD[name])
+    assert lib.sva_layer_norm(LayerNormParams(**{**NORM, "tokens": TOKENS}), t["x"], t["w"], t["b"], t["y"], t["mean"], t["rstd"], None) == BAD
+
+
+@pytest.mark.parametrize("name", NORM_BACKWARD)
+def test_layer_norm_gradients_apart(lib, name):
+    t = _norm(**NORM_BACKWARD[name])
+    p = LayerNormParams(**{**NORM, "tokens": TOKENS})
+    assert lib.sva_layer_norm_backward(p, t["dy"], t["x"], t["w"], t["mean"], t["rstd"], t["ws"], 1 << 20, t["dx"], t["dw"],
+                                       t["db"], None) == BAD
