@@ -183,7 +183,10 @@ void cross_attn_kernel(CrossArgs a) {
   wg_barrier();
   f32x4 sacc[2][QT];
   qk16<D>(sacc, &Ks[0][0], koff, qop);
-  if (seen[0] != ~0u) hide(sacc, seen[0], lane);
+  if (seen[0] != ~0u) {
+    settle(sacc[0], sacc[1]);
+    hide(sacc, seen[0], lane);
+  }
 
   // A step is one tile of keys, in stage st: its softmax and product with V, and S of the
   // tile after it, which past the last is the first one again for the next row tile.
@@ -314,6 +317,7 @@ __global__ __launch_bounds__(kThreads) void cross_few_kernel(CrossArgs a) {
     const unsigned char* kt = mine + st * 2 * CT;
     f32x4 s[2][1];
     qk16<D>(s, kt, koff, qop);
+    settle(s[0], s[1]);
     if (seen[0] != ~0u) hide(s, seen[0], lane);
     rs.follow(s, sl2);
     bf16x8 pop[1];

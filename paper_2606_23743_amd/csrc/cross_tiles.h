@@ -74,7 +74,9 @@ __device__ __forceinline__ void rows_times_half(f32x4 (&s)[QT], unsigned tile, c
   }
 }
 
-// eight wait states between products and whatever reads them
+// Eight wait states between products and whatever reads them: vector instructions may read a
+// product so much after its last instruction, and where a branch comes between, the compiler has
+// left them out.
 template <int QT>
 __device__ __forceinline__ void settle(f32x4 (&x)[QT], f32x4 (&y)[QT]) {
   if constexpr (QT == 1) asm volatile("s_nop 7" : "+v"(x[0]), "+v"(y[0]));
