@@ -194,6 +194,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, unit_offset: bool = Fals
     rg, rx = _rows(dy, dt, shp, "dy", dev), _rows(x, dt, shp, "x", dev)
     if dx is None:
         dx = _output(stream, torch.empty_like, x)
+    ro = _rows(dx, dt, shp, "dx", dev)
     sums = (B, C) if per else (C,)
     if want_weight and dweight is None:
         dweight = _output(stream, torch.empty, sums, dtype=torch.float32, device=x.device)
@@ -205,17 +206,21 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, unit_offset: bool = Fals
         ws_bytes = workspace.numel()
         ws_ptr = _plain(workspace, torch.uint8, (ws_bytes,), "workspace", dev)
     elif dweight is not None or dbias is not None:
-        ws_bytes = _norm_bytes.get((B, N, C, per))
+        # with shared weights, entries whose rows follow each other are one, and need the sums of one
+        one = (not per and rg.stride_b == N * rg.stride_n and rx.stride_b == N * rx.stride_n
+               and ro.stride_b == N * ro.stride_n and B * N < 1 << 31)
+        key = (1, B * N, C, 0) if one else (B, N, C, per)
+        ws_bytes = _norm_bytes.get(key)
         if ws_bytes is None:
             if len(_norm_bytes) > 4096:
                 _norm_bytes.clear()
-            ws_bytes = _norm_bytes[B, N, C, per] = layer_norm_backward_workspace(B, N, C, bool(per))
+            ws_bytes = _norm_bytes[key] = layer_norm_backward_workspace(*key)
         if ws_bytes:
             workspace = _scratch(stream, ws_bytes, x.device)
             ws_ptr = workspace.data_ptr()
     _check(_lib.load().sva_layer_norm_backward(
         prm, rg, rx, w, _plain(mean, torch.float32, (B, N), "mean", dev), _plain(rstd, torch.float32, (B, N), "rstd", dev),
-        ws_ptr, ws_bytes, _rows(dx, dt, shp, "dx", dev),
+        ws_ptr, ws_bytes, ro,
         None if dweight is None else _plain(dweight, torch.float32, sums, "dweight", dev),
         None if dbias is None else _plain(dbias, torch.float32, sums, "dbias", dev), _stream_on(stream, dev)),
         "sva_layer_norm_backward")

@@ -210,7 +210,7 @@ int sva_layer_norm(const sva_layer_norm_params* p, const sva_rows* x, const void
   return hip_status(sva::launch_layer_norm(a, s, static_cast<hipStream_t>(stream)));
 }
 
-// The most that any strides need: entries apart, or as one.
+// The most that any strides need: entries apart (one row each is a pitch of its own), or as one.
 int sva_layer_norm_backward_workspace(const sva_layer_norm_params* p, size_t* bytes) {
   if (!bytes) return SVA_ERR_INVALID_ARG;
   int st = check_norm(p);
@@ -218,7 +218,8 @@ int sva_layer_norm_backward_workspace(const sva_layer_norm_params* p, size_t* by
   sva::NormArgs a{};
   sva::NormShape s;
   size_t most = 0;
-  for (int joined = 0; joined <= (p->per_entry ? 0 : 1); ++joined) {
+  const int first = !p->per_entry && (p->batch == 1 || p->tokens == 1);
+  for (int joined = first; joined <= (p->per_entry ? 0 : 1); ++joined) {
     st = norm_sizes(p, joined != 0, true, &a, &s);       // (as one, any sizes will do)
     if (st == SVA_OK) most = std::max(most, s.ws_bytes);
   }
