@@ -17,9 +17,9 @@
 // Bound by the step's chain of S, softmax and product at the clock the power limit leaves,
 // and by the rows' traffic, which with few keys comes on top of it: 63,240 rows of 32 heads
 // of 128 over 512 keys 680 us (780 TFLOP/s; 1.04 GB), 16,384 rows of 4 heads over as many keys
-// 540 us (1,020 TFLOP/s), 32,760 rows of 2 x 20 heads of 112 over 512 keys with a mask
-// 440 us.  Few rows are bound by HBM: 2 x 7 tokens of 48 heads over 111,600 keys 173 us (5.3
-// TB/s).
+// 540 us (1,020 TFLOP/s), 32,760 rows of 2 x 20 heads of 112 over 512 keys 450 us, with a
+// tenth of them hidden by holes in a mask 510.  Few rows are bound by HBM: 2 x 7 tokens of 48
+// heads over 111,600 keys 173 us (5.3 TB/s).
 #include "cross_tiles.h"
 
 namespace sva {
